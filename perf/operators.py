@@ -174,12 +174,12 @@ def _plain_gate(s):
 def _own(s):
     import paper_1806_03461_amd as T
     if s["op"] == "linear":
-        T.clear_linear_i8(s["x"], s["w"], s["to"], x_scale=s["x_scale"], w_scale=s["w_scale"], bias=s["bias"])
+        T.bnn_dense_clear(s["x"], s["w"], s["to"], x_scale=s["x_scale"], w_scale=s["w_scale"], bias=s["bias"])
         return s["to"]
     if s["op"] == "norm":
-        T.clear_rms_norm_i8(s["x"], s["weight"], EPS, s["q"], s["scale"], residual=s["residual"], total=s.get("sum"))
+        T.bnn_rms_norm_clear(s["x"], s["weight"], EPS, s["q"], s["scale"], residual=s["residual"], total=s.get("sum"))
     else:
-        T.clear_gate_i8(s["gate"], s["up"], s["act"], s["q"], s["scale"])
+        T.bnn_gate_clear(s["gate"], s["up"], s["act"], s["q"], s["scale"])
     torch.mul(s["q"], s["scale"][:, None], out=s["values"])
     got = {"values": s["values"], "scale": s["scale"]}
     if "sum" in s:

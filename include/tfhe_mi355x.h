@@ -266,6 +266,52 @@ int bnn_conv_encrypted(tfhe_cloud_key *ck, const uint32_t *x, int C, int H, int 
                        const int8_t *K, int O, int kh, int kw, int stride, int pad,
                        const int32_t *T, uint32_t *out, void *stream);
 
+/* ---- layers in the clear, in 8-bit integers ------------------------------------------ */
+
+/* The clear side of a network: layers in front of the bits that a client encrypts, the clear form of a layer that is
+ * evaluated on ciphertexts (to choose its thresholds and to check decrypted answers), layers behind decrypted scores.
+ * These calls take no key.  All arrays are DEVICE memory of the current device.  A matrix is [rows][row stride] with
+ * neighbouring values of a row next to each other; strides count elements, are at least the row's length, and need no
+ * alignment beyond an element's; values between rows are neither read for the result nor written.  A call enqueues one kernel on
+ * `stream`, allocates and keeps nothing, and may be captured into a graph; calls on different streams do not share
+ * anything.  Outputs must not overlap inputs, but for `total` below.  Zero rows or channels are a no-op.  The same call on
+ * the same data gives the same bytes each time; a product's do not depend on the other rows of its operands. */
+enum { BNN_CLEAR_F32 = 0, BNN_CLEAR_BF16 = 1, BNN_CLEAR_F16 = 2,
+       BNN_CLEAR_I32 = 3,    /* int32 */
+       BNN_CLEAR_SIGN = 4,   /* int8: +1 or -1 */
+       BNN_CLEAR_BITS = 5    /* uint8: 1 or 0, what tfhe_encrypt takes */ };
+enum { BNN_ACT_IDENTITY = 0, BNN_ACT_RELU = 1, BNN_ACT_SILU = 2, BNN_ACT_GELU = 3 /* the exact one, with erf */ };
+
+/* A fully connected layer: acc[i][j] = sum over k of x[i][k] w[j][k] in exact integers (x: [m][k], w: [n][k]; k <= 131,071,
+ * else TFHE_E_SIZE), and by `kind`
+ *   F32, BF16, F16   out = acc * x_scale[i] * w_scale[j] + bias[j], in f32, rounded once to the output's type; a NULL
+ *                    scale is 1, bias is float[n] or NULL
+ *   I32              out = acc + bias[j] modulo 2^32; bias is int32[n] or NULL
+ *   SIGN, BITS       [acc + bias[j] >= 0], z = sign(Wx + b) with sign(0) = +1 (Sec. 3.2), without overflow; bias as for I32.
+ *                    With x in +-1 and w in {-1, 0, +1} this is bnn_dense_encrypted in the clear: bias = d - 2 T, where d
+ *                    is the row's number of non-zero weights.
+ * The last three take no scales (TFHE_E_PARAM).  k = 0 gives the bias. */
+int bnn_dense_clear(const int8_t *x, int64_t ldx, const int8_t *w, int64_t ldw, const float *x_scale,
+                    const float *w_scale, const void *bias, void *out, int64_t ldo, int kind, int64_t m, int64_t n,
+                    int64_t k, void *stream);
+
+/* Root-mean-square norm of rows, in 8 bits with a scale a row, what the product above takes:
+ *   h = x + residual (f32);  y = h / sqrt(mean of h^2 + eps) * weight;  scale[i] = max |y| / 127;  q = y / scale[i] rounded to the
+ *   nearest whole number, ties to even.
+ * x, residual, weight and total are of one type (F32, BF16 or F16); residual NULL: none; weight ([k]) NULL: ones; total, if not NULL,
+ * receives h rounded to the type, and may be x or residual itself (same pointer and stride).  The norm is that of the unrounded h.
+ * eps > 0.  k <= 65,536.  A row of zeros has scale 0 and q = 0.  A row in which h or h * weight leaves the f32 range or is
+ * NaN has a scale that is not finite and q = 0: a product with it is not a number. */
+int bnn_rms_norm_clear(const void *x, int64_t ldx, const void *residual, int64_t ldr, const void *weight, float eps,
+                       void *total, int64_t ldt, int8_t *q, int64_t ldq, float *scale, int type, int64_t m, int64_t k,
+                       void *stream);
+
+/* What stands between the two products of a gated feed-forward block: y = act(gate) * up in f32, or act(gate) if up is NULL, to 8 bits
+ * with a scale a row as above.  gate and up may be the two halves of one product's output.  With BNN_ACT_IDENTITY
+ * and no up this turns rows of numbers into what the product takes.  k <= 65,536. */
+int bnn_gate_clear(const void *gate, int64_t ldg, const void *up, int64_t ldu, int act, int8_t *q, int64_t ldq,
+                   float *scale, int type, int64_t m, int64_t k, void *stream);
+
 /* ---- measurement helpers ---------------------------------------------------------- */
 
 /* Kernel-time accounting of server-side calls on a cloud key: when enabled, the blind rotation

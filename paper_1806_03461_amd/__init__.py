@@ -16,6 +16,8 @@ LIB_PATH = os.path.join(HERE, "libtfhe_mi355x.so")
 NAND, AND, OR, NOR, XOR, XNOR, MUX, MUX_ELSE = range(8)
 OPS = {"NAND": NAND, "AND": AND, "OR": OR, "NOR": NOR, "XOR": XOR, "XNOR": XNOR}
 LOWER_DEFAULT, LOWER_MUX_COMPARATOR, LOWER_PLUS_ONE, LOWER_SHARE_GATES, LOWER_SORTING_NETWORK = 0, 1, 2, 4, 8
+CLEAR_F32, CLEAR_BF16, CLEAR_F16, CLEAR_I32, CLEAR_SIGN, CLEAR_BITS = range(6)
+ACTS = {"identity": 0, "relu": 1, "silu": 2, "gelu": 3}
 KEY_LWE_SK, KEY_TRLWE_SK, KEY_BK_RAW, KEY_KSK_RAW = range(4)
 
 GATE_DTYPE = np.dtype([("op", "u1"), ("neg0", "u1"), ("neg1", "u1"), ("pad", "u1"),
@@ -54,7 +56,8 @@ EXPORTS = ["tfhe_last_error", "tfhe_default_params", "tfhe_keygen", "tfhe_encryp
            "bnn_conv_lower_opts", "bnn_dense_encrypted", "bnn_dense_encrypted_opts", "bnn_conv_encrypted_opts",
            "bnn_conv_encrypted", "tfhe_profile_enable", "tfhe_profile_read", "tfhe_last_layer_stats", "tfhe_plan_wire_pool",
            "tfhe_measure_fp64_peak",
-           "tfhe_rounding_margin_enable", "tfhe_rounding_margin_read"]
+           "tfhe_rounding_margin_enable", "tfhe_rounding_margin_read",
+           "bnn_dense_clear", "bnn_rms_norm_clear", "bnn_gate_clear"]
 
 _lib = None
 
@@ -105,6 +108,10 @@ def lib():
         L.tfhe_profile_read.argtypes = [vp, C.POINTER(Profile), i32]
         L.tfhe_rounding_margin_enable.argtypes = [vp, i32]
         L.tfhe_rounding_margin_read.argtypes = [vp, C.POINTER(C.c_double)]
+        i64 = C.c_int64
+        L.bnn_dense_clear.argtypes = [vp, i64, vp, i64, vp, vp, vp, vp, i64, i32, i64, i64, i64, vp]
+        L.bnn_rms_norm_clear.argtypes = [vp, i64, vp, i64, vp, C.c_float, vp, i64, vp, i64, vp, i32, i64, i64, vp]
+        L.bnn_gate_clear.argtypes = [vp, i64, vp, i64, i32, vp, i64, vp, i32, i64, i64, vp]
         _lib = L
     return _lib
 
@@ -332,6 +339,90 @@ def bnn_conv_encrypted(ck, x, C_, H, Wd, K, T, stride, pad, out, stream=None):
     O, _, kh, kw = K.shape
     _check(lib().bnn_conv_encrypted(ck.handle, _dev_ptr(x), C_, H, Wd, K.ctypes.data, O, kh, kw, stride, pad,
                                     T.ctypes.data, _dev_ptr(out), _stream(stream)))
+
+
+# ---- layers in the clear, in 8-bit integers -----------------------------------------------------
+# Operands are torch tensors on the current device; rows may be strided, values of a row are neighbours.
+
+def _clear_kinds():
+    import torch
+    return {torch.float32: CLEAR_F32, torch.bfloat16: CLEAR_BF16, torch.float16: CLEAR_F16,
+            torch.int32: CLEAR_I32, torch.int8: CLEAR_SIGN, torch.uint8: CLEAR_BITS}
+
+
+_kinds = None
+
+
+def _matrix(name, t, dtype, rows, width, device):
+    """Device pointer and row stride of a [rows][width] tensor."""
+    if t.dtype != dtype or t.shape != (rows, width) or t.device != device:
+        raise ValueError(f"{name} must be a {rows} x {width} tensor of {dtype} on {device}, "
+                         f"not {tuple(t.shape)} of {t.dtype} on {t.device}")
+    step, nxt = t.stride()
+    if (nxt != 1 and width > 1) or (step < width and rows > 1):
+        raise ValueError(f"{name}: values of a row must be neighbours and rows must not overlap")
+    return t.data_ptr(), step if rows > 1 and step > width else width
+
+
+def _vector(name, t, dtype, size, device):
+    if t is None:
+        return None
+    if t.dtype != dtype or t.shape != (size,) or t.device != device or (size > 1 and t.stride(0) != 1):
+        raise ValueError(f"{name} must be {size} neighbouring values of {dtype} on {device}")
+    return t.data_ptr()
+
+
+def _clear_operand(name, t):
+    """Rows, width, device and output kind of a call's leading operand."""
+    global _kinds
+    if _kinds is None:
+        _kinds = _clear_kinds()
+    import torch
+    if not t.is_cuda or t.dim() != 2:
+        raise ValueError(f"{name} must be a matrix on the GPU")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, which is not the current device")
+    return t.shape[0], t.shape[1], t.device, _kinds.get(t.dtype, -1)
+
+
+def bnn_dense_clear(x, w, out, x_scale=None, w_scale=None, bias=None, stream=None):
+    """out = x w^T: x int8 [m][k], w int8 [n][k]; the kind of output goes by out's type (float32, bfloat16,
+    float16; int32 sums, int8 signs, uint8 bits).  bias: float32 [n] for the first three, int32 [n] otherwise."""
+    import torch
+    m, n, device, kind = _clear_operand("out", out)
+    if x.dim() != 2:
+        raise ValueError("x must be a matrix")
+    k = x.shape[1]
+    po, ldo = _matrix("out", out, out.dtype, m, n, device)
+    px, ldx = _matrix("x", x, torch.int8, m, k, device)
+    pw, ldw = _matrix("w", w, torch.int8, n, k, device)
+    _check(lib().bnn_dense_clear(px, ldx, pw, ldw, _vector("x_scale", x_scale, torch.float32, m, device),
+                                 _vector("w_scale", w_scale, torch.float32, n, device),
+                                 _vector("bias", bias, torch.int32 if kind >= CLEAR_I32 else torch.float32, n, device),
+                                 po, ldo, kind, m, n, k, _stream(stream)))
+
+
+def bnn_rms_norm_clear(x, weight, eps, q, scale, residual=None, total=None, stream=None):
+    """q, scale = rows of (x + residual) / rms * weight in 8 bits; total receives x + residual."""
+    import torch
+    m, k, device, kind = _clear_operand("x", x)
+    px, ldx = _matrix("x", x, x.dtype, m, k, device)
+    pr, ldr = (None, k) if residual is None else _matrix("residual", residual, x.dtype, m, k, device)
+    pt, ldt = (None, k) if total is None else _matrix("total", total, x.dtype, m, k, device)
+    pq, ldq = _matrix("q", q, torch.int8, m, k, device)
+    _check(lib().bnn_rms_norm_clear(px, ldx, pr, ldr, _vector("weight", weight, x.dtype, k, device), eps, pt, ldt, pq,
+                                    ldq, _vector("scale", scale, torch.float32, m, device), kind, m, k, _stream(stream)))
+
+
+def bnn_gate_clear(gate, up, act, q, scale, stream=None):
+    """q, scale = rows of act(gate) * up in 8 bits; up None: act(gate) alone.  act: a name of ACTS."""
+    import torch
+    m, k, device, kind = _clear_operand("gate", gate)
+    pg, ldg = _matrix("gate", gate, gate.dtype, m, k, device)
+    pu, ldu = (None, k) if up is None else _matrix("up", up, gate.dtype, m, k, device)
+    pq, ldq = _matrix("q", q, torch.int8, m, k, device)
+    _check(lib().bnn_gate_clear(pg, ldg, pu, ldu, ACTS[act], pq, ldq, _vector("scale", scale, torch.float32, m, device),
+                                kind, m, k, _stream(stream)))
 
 
 def tfhe_plan_wire_pool(gates, nwires, n_fixed, outs):

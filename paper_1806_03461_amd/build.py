@@ -12,7 +12,7 @@ LIB = os.path.join(HERE, "libtfhe_mi355x.so")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wall", "-Wno-unused-command-line-argument", "-Wno-unknown-attributes"]
-SOURCES = ["host_keys.cpp", "executor.cpp", "bnn_lower.cpp", "kernels.hip"]
+SOURCES = ["host_keys.cpp", "executor.cpp", "bnn_lower.cpp", "clear_layers.cpp", "kernels.hip", "clear_kernels.hip"]
 
 
 def build(verbose: bool = False) -> str:

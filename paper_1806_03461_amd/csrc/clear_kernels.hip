@@ -1,13 +1,15 @@
 // gfx950 kernels of layers in the clear: the 8-bit matrix product, and the two row operators that feed it (norm, gated activation).
 #include "clear_kernels.h"
 
+#include <type_traits>
+
 #include <hip/hip_bf16.h>
 #include <hip/hip_fp16.h>
 
 namespace tfhe {
 
 typedef int v4i __attribute__((ext_vector_type(4)));
-typedef float v4f __attribute__((ext_vector_type(4)));
+typedef int v16i __attribute__((ext_vector_type(16)));
 
 // ---- the product ---------------------------------------------------------------------------------------------------
 
@@ -23,83 +25,276 @@ __device__ __forceinline__ v4i load_16(const int8_t *row, int at, int k) {
     return v;
 }
 
-template <int KIND>
-__device__ __forceinline__ void store_out(const DenseClearArgs &a, int64_t i, int64_t j, int acc) {
-    const int64_t at = i * a.ldo + j;
-    if constexpr (KIND >= BNN_CLEAR_I32) {
-        const int b = a.bias ? static_cast<const int *>(a.bias)[j] : 0;
-        if constexpr (KIND == BNN_CLEAR_I32) {
-            static_cast<int *>(a.out)[at] = (int)((unsigned)acc + (unsigned)b);
-        } else {
-            const bool one = (int64_t)acc + b >= 0;
-            if constexpr (KIND == BNN_CLEAR_SIGN) static_cast<int8_t *>(a.out)[at] = one ? 1 : -1;
-            else static_cast<uint8_t *>(a.out)[at] = one;
-        }
+// v[0 .. 3] = p[0 .. left - 1], the rest as they are
+template <class T>
+__device__ __forceinline__ void load_4(T (&v)[4], const T *p, int left) {
+    if (left == 4) {
+        __builtin_memcpy(v, p, sizeof v);
     } else {
-        float y = (float)acc;
-        if (a.x_scale) y *= a.x_scale[i];
-        if (a.w_scale) y *= a.w_scale[j];
-        if (a.bias) y += static_cast<const float *>(a.bias)[j];
-        if constexpr (KIND == BNN_CLEAR_F32) static_cast<float *>(a.out)[at] = y;
-        else if constexpr (KIND == BNN_CLEAR_BF16) static_cast<__hip_bfloat16 *>(a.out)[at] = __float2bfloat16(y);
-        else static_cast<__half *>(a.out)[at] = __float2half(y);
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+            if (e < left) v[e] = p[e];
     }
 }
 
-// 64 tokens by 64 channels a workgroup of four waves, each 32 by 32; 64 bytes of k at a time through LDS.
-template <int KIND>
-__global__ void __launch_bounds__(256) dense_tile_kernel(DenseClearArgs a) {
-    __shared__ v4i xs[64][5], ws[64][5];
-    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-    const int64_t across = (a.n + 63) / 64, tiles = across * ((a.m + 63) / 64);
-    for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        const int64_t i0 = tile / across * 64, j0 = tile % across * 64;
-        const int row = t >> 2, part = t & 3;
-        const int64_t xi = i0 + row < a.m ? i0 + row : a.m - 1, wj = j0 + row < a.n ? j0 + row : a.n - 1;
-        v4i acc[2][2] = {};
-        for (int k0 = 0; k0 < a.k; k0 += 64) {
-            const v4i x = load_16(a.x + xi * a.ldx, k0 + 16 * part, a.k), w = load_16(a.w + wj * a.ldw, k0 + 16 * part, a.k);
-            __syncthreads();
-            xs[row][part] = x;
-            ws[row][part] = w;
-            __syncthreads();
-            v4i fx[2], fw[2];
-            for (int r = 0; r < 2; ++r) {
-                fx[r] = xs[(wave >> 1) * 32 + 16 * r + (lane & 15)][lane >> 4];
-                fw[r] = ws[(wave & 1) * 32 + 16 * r + (lane & 15)][lane >> 4];
-            }
-            for (int r = 0; r < 2; ++r)
-                for (int c = 0; c < 2; ++c) acc[r][c] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[c], fx[r], acc[r][c], 0, 0, 0);
+template <class T>
+__device__ __forceinline__ void store_4(T *p, const T (&v)[4], int left) {
+    if (left == 4) {
+        __builtin_memcpy(p, v, sizeof v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+            if (e < left) p[e] = v[e];
+    }
+}
+
+// The outputs of four neighbouring channels of token i, j .. j + 3, of which those below n exist, from their sums.
+__device__ __forceinline__ void finish_4(const DenseClearArgs &a, int64_t i, int64_t j, v4i acc) {
+    const int left = a.n - j < 4 ? (int)(a.n - j) : 4;
+    const int64_t at = i * a.ldo + j;
+    if (a.kind >= BNN_CLEAR_I32) {
+        int b[4] = {0, 0, 0, 0};
+        if (a.bias) load_4(b, static_cast<const int *>(a.bias) + j, left);
+        if (a.kind == BNN_CLEAR_I32) {
+            int o[4];
+            for (int e = 0; e < 4; ++e) o[e] = (int)((unsigned)acc[e] + (unsigned)b[e]);
+            store_4(static_cast<int *>(a.out) + at, o, left);
+        } else {
+            const int8_t no = a.kind == BNN_CLEAR_SIGN ? -1 : 0;
+            int8_t o[4];
+            for (int e = 0; e < 4; ++e) o[e] = (int64_t)acc[e] + b[e] >= 0 ? (int8_t)1 : no;
+            store_4(static_cast<int8_t *>(a.out) + at, o, left);
         }
-        for (int r = 0; r < 2; ++r)
-            for (int c = 0; c < 2; ++c)
-                for (int e = 0; e < 4; ++e) {
-                    const int64_t i = i0 + (wave >> 1) * 32 + 16 * r + (lane & 15);
-                    const int64_t j = j0 + (wave & 1) * 32 + 16 * c + 4 * (lane >> 4) + e;
-                    if (i < a.m && j < a.n) store_out<KIND>(a, i, j, acc[r][c][e]);
+        return;
+    }
+    float sw[4] = {1.0f, 1.0f, 1.0f, 1.0f}, b[4] = {0.0f, 0.0f, 0.0f, 0.0f}, y[4];
+    const float sx = a.x_scale ? a.x_scale[i] : 1.0f;
+    if (a.w_scale) load_4(sw, a.w_scale + j, left);
+    if (a.bias) load_4(b, static_cast<const float *>(a.bias) + j, left);
+    for (int e = 0; e < 4; ++e) y[e] = (float)acc[e] * sx * sw[e] + b[e];
+    if (a.kind == BNN_CLEAR_F32) {
+        store_4(static_cast<float *>(a.out) + at, y, left);
+    } else if (a.kind == BNN_CLEAR_BF16) {
+        __hip_bfloat16 o[4];
+        for (int e = 0; e < 4; ++e) o[e] = __float2bfloat16(y[e]);
+        store_4(static_cast<__hip_bfloat16 *>(a.out) + at, o, left);
+    } else {
+        __half o[4];
+        for (int e = 0; e < 4; ++e) o[e] = __float2half(y[e]);
+        store_4(static_cast<__half *>(a.out) + at, o, left);
+    }
+}
+
+// Waits until at most `left` of the wave's loads into LDS are under way and its reads of LDS have come, then meets the workgroup.
+template <int left>
+__device__ __forceinline__ void landed_and_meet() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(left) : "memory");
+}
+
+// Tiles of (WT * RT * 32) tokens by (WC * RC * 32) channels, a workgroup of WT x WC waves each, every wave RT x RC products of 32 by 32.
+// 128 bytes of k at a time go through LDS, the next 128 under way while these are multiplied.  A row's eight 16-byte pieces lie in
+// LDS at place (piece ^ row % 8), so that the eight lanes that read one piece of eight rows meet all banks.
+// The channels are the products' rows: a lane then holds four neighbouring channels of a token.
+//   ALIGNED: rows begin at multiples of 16 bytes and k is one too; pieces go from memory to LDS directly.  Otherwise through registers.
+template <int WT, int WC, int RT, int RC, bool ALIGNED>
+__global__ void __launch_bounds__(64 * WT * WC, 2) dense_tile_kernel(DenseClearArgs a) {
+    constexpr int kThreads = 64 * WT * WC, kWaves = WT * WC, TT = 32 * WT * RT, TC = 32 * WC * RC;
+    constexpr int kPieces = (TT + TC) * 8 / kThreads;       // of 16 bytes, a thread
+    constexpr int kXPieces = TT * 8 / kThreads;
+    constexpr int kRow = 32 * RC + 4;                       // words of a token's channels as the sums pass through LDS
+    static_assert(kWaves * 32 * kRow * 4 <= 2 * (TT + TC) * 128, "the sums pass through the operands' LDS");
+    static_assert(kXPieces * kThreads == TT * 8 && kPieces * kThreads == (TT + TC) * 8, "whole pieces a thread");
+    __shared__ __attribute__((aligned(1024))) int8_t lds[2][(TT + TC) * 128];
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int64_t across = (a.n + TC - 1) / TC, down = (a.m + TT - 1) / TT, tiles = across * down;
+    const int steps = (a.k + 127) / 128;
+    for (int64_t id = blockIdx.x; id < tiles; id += gridDim.x) {
+        // Workgroups go round the eight XCDs; each XCD gets neighbouring tiles, four token tiles by all channels at a time, so that
+        // its L2 is asked for the same rows.
+        const int64_t xcd = id & 7, share = tiles >> 3, over = tiles & 7;
+        const int64_t lin = xcd * share + (xcd < over ? xcd : over) + (id >> 3);
+        const int64_t band = lin / (4 * across), in_band = lin - band * 4 * across, first = band * 4, high = down - first < 4 ? down - first : 4;
+        const int64_t i0 = (first + in_band % high) * TT, j0 = in_band / high * TC;
+
+        // piece p of a thread: row p * kThreads / 8 + t / 8 of the tile's tokens, then of its channels
+        const int place = t & 7, row8 = t >> 3, piece = place ^ (row8 & 7);
+        const int8_t *row[kPieces];
+        int offset[kPieces];
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p) {
+            const bool is_x = p < kXPieces;
+            const int64_t r = (is_x ? i0 : j0) + (p - (is_x ? 0 : kXPieces)) * (kThreads / 8) + row8, rows = is_x ? a.m : a.n;
+            const int64_t kept = r < rows ? r : rows - 1;       // beyond the last row: that row again, never stored
+            if (ALIGNED) offset[p] = (int)((kept - (is_x ? i0 : j0)) * (is_x ? a.ldx : a.ldw)) + 16 * piece;
+            else row[p] = is_x ? a.x + kept * a.ldx : a.w + kept * a.ldw;
+        }
+        const int64_t x_end = ((a.m - i0 < TT ? a.m - i0 : TT) - 1) * a.ldx + a.k, w_end = ((a.n - j0 < TC ? a.n - j0 : TC) - 1) * a.ldw + a.k;
+        const auto xr = __builtin_amdgcn_make_buffer_rsrc((void *)(a.x + i0 * a.ldx), (short)0, (int)x_end, 0x00020000);
+        const auto wr = __builtin_amdgcn_make_buffer_rsrc((void *)(a.w + j0 * a.ldw), (short)0, (int)w_end, 0x00020000);
+        v4i held[ALIGNED ? 1 : kPieces];
+        const auto fetch = [&](int s, int8_t *to) {
+#pragma unroll
+            for (int p = 0; p < kPieces; ++p) {
+                if constexpr (ALIGNED) {
+                    // a piece beyond k: an offset beyond the buffer, which reads as 0
+                    const int at = 128 * s + 16 * piece < a.k ? offset[p] : (int)0x80000000;
+                    const auto lds_at = (__attribute__((address_space(3))) void *)(to + p * 16 * kThreads + 1024 * wave);
+                    if (p < kXPieces) __builtin_amdgcn_raw_ptr_buffer_load_lds(xr, lds_at, 16, at, 128 * s, 0, 0);
+                    else __builtin_amdgcn_raw_ptr_buffer_load_lds(wr, lds_at, 16, at, 128 * s, 0, 0);
+                } else {
+                    held[p] = load_16(row[p], 128 * s + 16 * piece, a.k);
                 }
+            }
+        };
+        const auto settle = [&](int8_t *to) {
+            if constexpr (!ALIGNED) {
+#pragma unroll
+                for (int p = 0; p < kPieces; ++p) *reinterpret_cast<v4i *>(to + (p * kThreads + t) * 16) = held[p];
+            }
+        };
+
+        v16i acc[RT][RC] = {};
+        const int at_x = (wave / WC) * 32 * RT + (lane & 31), at_w = TT + (wave % WC) * 32 * RC + (lane & 31);
+        if (steps > 0) {
+            fetch(0, lds[0]);
+            settle(lds[0]);
+        }
+        landed_and_meet<0>();
+        for (int s = 0; s < steps; ++s) {
+            const int8_t *from = lds[s & 1];
+            if (s + 1 < steps) fetch(s + 1, lds[(s + 1) & 1]);
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) {
+                const int where = 16 * ((2 * kk + (lane >> 5)) ^ (lane & 7));
+                v4i fx[RT], fw[RC];
+#pragma unroll
+                for (int r = 0; r < RT; ++r) fx[r] = *reinterpret_cast<const v4i *>(from + (at_x + 32 * r) * 128 + where);
+#pragma unroll
+                for (int c = 0; c < RC; ++c) fw[c] = *reinterpret_cast<const v4i *>(from + (at_w + 32 * c) * 128 + where);
+#pragma unroll
+                for (int r = 0; r < RT; ++r)
+#pragma unroll
+                    for (int c = 0; c < RC; ++c) acc[r][c] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fw[c], fx[r], acc[r][c], 0, 0, 0);
+            }
+            if (s + 1 < steps) settle(lds[(s + 1) & 1]);
+            landed_and_meet<0>();
+        }
+        // The wave's sums go through LDS of its own, 32 tokens at a time, so that its stores are whole stretches of a token's channels.
+        int *own = reinterpret_cast<int *>(&lds[0][0]) + wave * 32 * kRow;
+        const int64_t wave_i = i0 + (wave / WC) * 32 * RT, wave_j = j0 + (wave % WC) * 32 * RC;
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+#pragma unroll
+            for (int c = 0; c < RC; ++c)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const v4i four = {acc[r][c][4 * e], acc[r][c][4 * e + 1], acc[r][c][4 * e + 2], acc[r][c][4 * e + 3]};
+                    *reinterpret_cast<v4i *>(own + (lane & 31) * kRow + 32 * c + 8 * e + 4 * (lane >> 5)) = four;
+                }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+            for (int at = lane; at < 32 * 8 * RC; at += 64) {
+                const int64_t i = wave_i + 32 * r + at / (8 * RC), j = wave_j + 4 * (at % (8 * RC));
+                if (i < a.m && j < a.n) finish_4(a, i, j, *reinterpret_cast<const v4i *>(own + at / (8 * RC) * kRow + 4 * (at % (8 * RC))));
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+        __syncthreads();
+    }
+}
+
+// Few tokens (up to 16 RT): the weights are read once and that is what it costs.  A workgroup takes 16 channels, its eight waves
+// 64-byte blocks of k in turn; the weights go from memory to the products' registers without LDS, the waves' sums meet there.
+template <int RT>
+__global__ void __launch_bounds__(512) dense_few_kernel(DenseClearArgs a) {
+    constexpr int kWaves = 8, kAhead = RT == 1 ? 8 : 4;
+    __shared__ v4i sums[kWaves][RT][64];
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int64_t groups = (a.n + 15) / 16;
+    const int blocks = a.k / 64, part = 16 * (lane >> 4);
+    for (int64_t group = blockIdx.x; group < groups; group += gridDim.x) {
+        const int64_t j = group * 16 + (lane & 15), kept = j < a.n ? j : a.n - 1;
+        const int8_t *w = a.w + kept * a.ldw + part;
+        const int8_t *x[RT];
+        for (int r = 0; r < RT; ++r) {
+            const int64_t i = 16 * r + (lane & 15);
+            x[r] = i < a.m ? a.x + i * a.ldx + part : nullptr;
+        }
+        v4i acc[RT] = {};
+        // wave w: blocks w * each ... of k, and the last wave what is left of less than a block
+        const int each = (blocks + kWaves - 1) / kWaves, last = (wave + 1) * each < blocks ? (wave + 1) * each : blocks;
+        for (int b = wave * each; b < last; b += kAhead) {
+            v4i fw[kAhead], fx[kAhead][RT];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const int at = 64 * (b + u < last ? b + u : last - 1);
+                __builtin_memcpy(&fw[u], w + at, 16);
+#pragma unroll
+                for (int r = 0; r < RT; ++r) {
+                    fx[u][r] = v4i{0, 0, 0, 0};
+                    if (x[r] && b + u < last) __builtin_memcpy(&fx[u][r], x[r] + at, 16);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+                for (int r = 0; r < RT; ++r) acc[r] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[u], fx[u][r], acc[r], 0, 0, 0);
+        }
+        if (wave == kWaves - 1 && blocks * 64 < a.k) {
+            const int at = blocks * 64 + part;
+            const v4i fw = load_16(w - part, at, a.k);
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                const v4i fx = x[r] ? load_16(x[r] - part, at, a.k) : v4i{0, 0, 0, 0};
+                acc[r] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw, fx, acc[r], 0, 0, 0);
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < RT; ++r) sums[wave][r][lane] = acc[r];
+        __syncthreads();
+        if (t < 64 * RT) {
+            const int r = t >> 6;
+            v4i s = sums[0][r][lane];
+            for (int v = 1; v < kWaves; ++v) s += sums[v][r][lane];
+            const int64_t i = 16 * r + (lane & 15), first = group * 16 + 4 * (lane >> 4);
+            if (i < a.m && first < a.n) finish_4(a, i, first, s);
+        }
         __syncthreads();
     }
 }
 
 // workgroups of a launch: more tiles or rows than this are taken in turn, so that no grid outgrows what a launch may have
 constexpr int64_t kMostGroups = 1 << 20;
+static dim3 groups_of(int64_t tiles) { return dim3((unsigned)(tiles < kMostGroups ? tiles : kMostGroups)); }
 
-template <int KIND>
+template <int WT, int WC, int RT, int RC>
+static void tile_launch(const DenseClearArgs &a, bool aligned, hipStream_t stream) {
+    const int64_t tiles = ((a.n + 32 * WC * RC - 1) / (32 * WC * RC)) * ((a.m + 32 * WT * RT - 1) / (32 * WT * RT));
+    if (aligned) dense_tile_kernel<WT, WC, RT, RC, true><<<groups_of(tiles), 64 * WT * WC, 0, stream>>>(a);
+    else dense_tile_kernel<WT, WC, RT, RC, false><<<groups_of(tiles), 64 * WT * WC, 0, stream>>>(a);
+}
+
 static void dense_launch(const DenseClearArgs &a, hipStream_t stream) {
-    const int64_t tiles = ((a.n + 63) / 64) * ((a.m + 63) / 64);
-    dense_tile_kernel<KIND><<<dim3((unsigned)(tiles < kMostGroups ? tiles : kMostGroups)), 256, 0, stream>>>(a);
+    // FORM-BEGIN
+    const auto sixteen = [](const void *p, int64_t ld) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 16 == 0 && ld <= 1 << 22; };
+    const bool aligned = a.k % 16 == 0 && sixteen(a.x, a.ldx) && sixteen(a.w, a.ldw);
+    const auto tiles = [&](int64_t side) { return ((a.m + side - 1) / side) * ((a.n + side - 1) / side); };
+    int form = a.m <= 16 ? 1 : a.m <= 32 ? 2 : a.m <= 64 ? 3 : tiles(256) >= 192 ? 6 : tiles(128) >= 192 ? 5 : 4;
+    // FORM-END
+    switch (form) {
+        case 1: dense_few_kernel<1><<<groups_of((a.n + 15) / 16), 512, 0, stream>>>(a); break;
+        case 2: dense_few_kernel<2><<<groups_of((a.n + 15) / 16), 512, 0, stream>>>(a); break;
+        case 3: dense_few_kernel<4><<<groups_of((a.n + 15) / 16), 512, 0, stream>>>(a); break;
+        case 4: tile_launch<2, 2, 1, 1>(a, aligned, stream); break;
+        case 5: tile_launch<2, 2, 2, 2>(a, aligned, stream); break;
+        default: tile_launch<2, 4, 4, 2>(a, aligned, stream); break;
+    }
 }
 
 int launch_dense_clear(const DenseClearArgs &a, hipStream_t stream) {
-    switch (a.kind) {
-        case BNN_CLEAR_F32: dense_launch<BNN_CLEAR_F32>(a, stream); break;
-        case BNN_CLEAR_BF16: dense_launch<BNN_CLEAR_BF16>(a, stream); break;
-        case BNN_CLEAR_F16: dense_launch<BNN_CLEAR_F16>(a, stream); break;
-        case BNN_CLEAR_I32: dense_launch<BNN_CLEAR_I32>(a, stream); break;
-        case BNN_CLEAR_SIGN: dense_launch<BNN_CLEAR_SIGN>(a, stream); break;
-        default: dense_launch<BNN_CLEAR_BITS>(a, stream); break;
-    }
+    dense_launch(a, stream);
     TFHE_HIP(hipGetLastError());
     return TFHE_OK;
 }
@@ -293,12 +488,11 @@ __global__ void __launch_bounds__(THREADS == 64 ? 256 : THREADS) rows_kernel(Row
 template <class T, bool NORM, int ACT>
 static void rows_launch(const RowsClearArgs &a, hipStream_t stream) {
     const int64_t chunks = (a.k + 7) / 8;
-    const auto groups = [&](int64_t rows) { return dim3((unsigned)(rows < kMostGroups ? rows : kMostGroups)); };
-    if (chunks <= 64) rows_kernel<T, NORM, ACT, 64, 1><<<groups((a.m + 3) / 4), 256, 0, stream>>>(a);
-    else if (chunks <= 256) rows_kernel<T, NORM, ACT, 256, 1><<<groups(a.m), 256, 0, stream>>>(a);
-    else if (chunks <= 1024) rows_kernel<T, NORM, ACT, 1024, 1><<<groups(a.m), 1024, 0, stream>>>(a);
-    else if (chunks <= 2048) rows_kernel<T, NORM, ACT, 1024, 2><<<groups(a.m), 1024, 0, stream>>>(a);
-    else rows_kernel<T, NORM, ACT, 1024, 8><<<groups(a.m), 1024, 0, stream>>>(a);
+    if (chunks <= 64) rows_kernel<T, NORM, ACT, 64, 1><<<groups_of((a.m + 3) / 4), 256, 0, stream>>>(a);
+    else if (chunks <= 256) rows_kernel<T, NORM, ACT, 256, 1><<<groups_of(a.m), 256, 0, stream>>>(a);
+    else if (chunks <= 1024) rows_kernel<T, NORM, ACT, 1024, 1><<<groups_of(a.m), 1024, 0, stream>>>(a);
+    else if (chunks <= 2048) rows_kernel<T, NORM, ACT, 1024, 2><<<groups_of(a.m), 1024, 0, stream>>>(a);
+    else rows_kernel<T, NORM, ACT, 1024, 8><<<groups_of(a.m), 1024, 0, stream>>>(a);
 }
 
 template <bool NORM, int ACT>

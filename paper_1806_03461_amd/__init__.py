@@ -342,87 +342,110 @@ def bnn_conv_encrypted(ck, x, C_, H, Wd, K, T, stride, pad, out, stream=None):
 
 
 # ---- layers in the clear, in 8-bit integers -----------------------------------------------------
-# Operands are torch tensors on the current device; rows may be strided, values of a row are neighbours.
+# Operands are torch tensors on the current device; rows may be strided, values of a row are neighbours.  A call of a few
+# microseconds is mostly this marshalling, so a tensor is looked at once and with the cheapest questions; torch's own
+# current_stream() alone takes 2.7 us, the handle it wraps 0.1.
 
-def _clear_kinds():
-    import torch
-    return {torch.float32: CLEAR_F32, torch.bfloat16: CLEAR_BF16, torch.float16: CLEAR_F16,
-            torch.int32: CLEAR_I32, torch.int8: CLEAR_SIGN, torch.uint8: CLEAR_BITS}
+class _Torch:
+    """What these calls need of torch, looked up at the first of them."""
+
+    def __init__(self):
+        import torch
+        self.device, self.stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+        self.i8, self.i32, self.f32 = torch.int8, torch.int32, torch.float32
+        self.kinds = {torch.float32: CLEAR_F32, torch.bfloat16: CLEAR_BF16, torch.float16: CLEAR_F16,
+                      torch.int32: CLEAR_I32, torch.int8: CLEAR_SIGN, torch.uint8: CLEAR_BITS}
 
 
-_kinds = None
+_torch = None
 
 
-def _matrix(name, t, dtype, rows, width, device):
+def _clear_call(name, t):
+    """Torch's part, and the device of a call's leading operand, which has to be the current one."""
+    global _torch
+    if _torch is None:
+        _torch = _Torch()
+    if not t.is_cuda or t.dim() != 2:
+        raise ValueError(f"{name} must be a matrix on the GPU")
+    device = t.get_device()
+    if device != _torch.device():
+        raise ValueError(f"{name} is on {t.device}, which is not the current device")
+    return _torch, device
+
+
+def _matrix(name, t, dtype, shape, device):
     """Device pointer and row stride of a [rows][width] tensor."""
-    if t.dtype != dtype or t.shape != (rows, width) or t.device != device:
-        raise ValueError(f"{name} must be a {rows} x {width} tensor of {dtype} on {device}, "
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device:
+        raise ValueError(f"{name} must be a {shape[0]} x {shape[1]} tensor of {dtype} on device {device}, "
                          f"not {tuple(t.shape)} of {t.dtype} on {t.device}")
+    if t.is_contiguous():
+        return t.data_ptr(), shape[1]
     step, nxt = t.stride()
-    if (nxt != 1 and width > 1) or (step < width and rows > 1):
+    if (nxt != 1 and shape[1] > 1) or (step < shape[1] and shape[0] > 1):
         raise ValueError(f"{name}: values of a row must be neighbours and rows must not overlap")
-    return t.data_ptr(), step if rows > 1 and step > width else width
+    return t.data_ptr(), step if shape[0] > 1 else shape[1]
 
 
 def _vector(name, t, dtype, size, device):
-    if t is None:
-        return None
-    if t.dtype != dtype or t.shape != (size,) or t.device != device or (size > 1 and t.stride(0) != 1):
-        raise ValueError(f"{name} must be {size} neighbouring values of {dtype} on {device}")
+    if t.dtype is not dtype or t.shape != (size,) or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{name} must be {size} neighbouring values of {dtype} on device {device}")
     return t.data_ptr()
-
-
-def _clear_operand(name, t):
-    """Rows, width, device and output kind of a call's leading operand."""
-    global _kinds
-    if _kinds is None:
-        _kinds = _clear_kinds()
-    import torch
-    if not t.is_cuda or t.dim() != 2:
-        raise ValueError(f"{name} must be a matrix on the GPU")
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} is on {t.device}, which is not the current device")
-    return t.shape[0], t.shape[1], t.device, _kinds.get(t.dtype, -1)
 
 
 def bnn_dense_clear(x, w, out, x_scale=None, w_scale=None, bias=None, stream=None):
     """out = x w^T: x int8 [m][k], w int8 [n][k]; the kind of output goes by out's type (float32, bfloat16,
     float16; int32 sums, int8 signs, uint8 bits).  bias: float32 [n] for the first three, int32 [n] otherwise."""
-    import torch
-    m, n, device, kind = _clear_operand("out", out)
-    if x.dim() != 2:
-        raise ValueError("x must be a matrix")
-    k = x.shape[1]
-    po, ldo = _matrix("out", out, out.dtype, m, n, device)
-    px, ldx = _matrix("x", x, torch.int8, m, k, device)
-    pw, ldw = _matrix("w", w, torch.int8, n, k, device)
-    _check(lib().bnn_dense_clear(px, ldx, pw, ldw, _vector("x_scale", x_scale, torch.float32, m, device),
-                                 _vector("w_scale", w_scale, torch.float32, n, device),
-                                 _vector("bias", bias, torch.int32 if kind >= CLEAR_I32 else torch.float32, n, device),
-                                 po, ldo, kind, m, n, k, _stream(stream)))
+    t, device = _clear_call("out", out)
+    m, n = out.shape
+    k = x.shape[-1] if x.dim() == 2 else -1
+    kind = t.kinds.get(out.dtype, -1)
+    po, ldo = _matrix("out", out, out.dtype, (m, n), device)
+    px, ldx = _matrix("x", x, t.i8, (m, k), device)
+    pw, ldw = _matrix("w", w, t.i8, (n, k), device)
+    if x_scale is not None:
+        x_scale = _vector("x_scale", x_scale, t.f32, m, device)
+    if w_scale is not None:
+        w_scale = _vector("w_scale", w_scale, t.f32, n, device)
+    if bias is not None:
+        bias = _vector("bias", bias, t.i32 if kind >= CLEAR_I32 else t.f32, n, device)
+    rc = (_lib or lib()).bnn_dense_clear(px, ldx, pw, ldw, x_scale, w_scale, bias, po, ldo, kind, m, n, k,
+                                         t.stream(device) if stream is None else stream)
+    if rc:
+        _check(rc)
 
 
 def bnn_rms_norm_clear(x, weight, eps, q, scale, residual=None, total=None, stream=None):
-    """q, scale = rows of (x + residual) / rms * weight in 8 bits; total receives x + residual."""
-    import torch
-    m, k, device, kind = _clear_operand("x", x)
-    px, ldx = _matrix("x", x, x.dtype, m, k, device)
-    pr, ldr = (None, k) if residual is None else _matrix("residual", residual, x.dtype, m, k, device)
-    pt, ldt = (None, k) if total is None else _matrix("total", total, x.dtype, m, k, device)
-    pq, ldq = _matrix("q", q, torch.int8, m, k, device)
-    _check(lib().bnn_rms_norm_clear(px, ldx, pr, ldr, _vector("weight", weight, x.dtype, k, device), eps, pt, ldt, pq,
-                                    ldq, _vector("scale", scale, torch.float32, m, device), kind, m, k, _stream(stream)))
+    """q, scale = rows of (x + residual) / rms * weight in 8 bits; weight None: ones; total receives x + residual."""
+    t, device = _clear_call("x", x)
+    shape, dtype = x.shape, x.dtype
+    m, k = shape
+    px, ldx = _matrix("x", x, dtype, shape, device)
+    pr, ldr = (None, k) if residual is None else _matrix("residual", residual, dtype, shape, device)
+    pt, ldt = (None, k) if total is None else _matrix("total", total, dtype, shape, device)
+    pq, ldq = _matrix("q", q, t.i8, shape, device)
+    if weight is not None:
+        weight = _vector("weight", weight, dtype, k, device)
+    rc = (_lib or lib()).bnn_rms_norm_clear(px, ldx, pr, ldr, weight, eps, pt, ldt, pq, ldq,
+                                            _vector("scale", scale, t.f32, m, device), t.kinds.get(dtype, -1), m, k,
+                                            t.stream(device) if stream is None else stream)
+    if rc:
+        _check(rc)
 
 
 def bnn_gate_clear(gate, up, act, q, scale, stream=None):
     """q, scale = rows of act(gate) * up in 8 bits; up None: act(gate) alone.  act: a name of ACTS."""
-    import torch
-    m, k, device, kind = _clear_operand("gate", gate)
-    pg, ldg = _matrix("gate", gate, gate.dtype, m, k, device)
-    pu, ldu = (None, k) if up is None else _matrix("up", up, gate.dtype, m, k, device)
-    pq, ldq = _matrix("q", q, torch.int8, m, k, device)
-    _check(lib().bnn_gate_clear(pg, ldg, pu, ldu, ACTS[act], pq, ldq, _vector("scale", scale, torch.float32, m, device),
-                                kind, m, k, _stream(stream)))
+    t, device = _clear_call("gate", gate)
+    shape, dtype = gate.shape, gate.dtype
+    m, k = shape
+    if act not in ACTS:
+        raise ValueError(f"act must be one of {', '.join(ACTS)}, not {act!r}")
+    pg, ldg = _matrix("gate", gate, dtype, shape, device)
+    pu, ldu = (None, k) if up is None else _matrix("up", up, dtype, shape, device)
+    pq, ldq = _matrix("q", q, t.i8, shape, device)
+    rc = (_lib or lib()).bnn_gate_clear(pg, ldg, pu, ldu, ACTS[act], pq, ldq, _vector("scale", scale, t.f32, m, device),
+                                        t.kinds.get(dtype, -1), m, k, t.stream(device) if stream is None else stream)
+    if rc:
+        _check(rc)
 
 
 def tfhe_plan_wire_pool(gates, nwires, n_fixed, outs):

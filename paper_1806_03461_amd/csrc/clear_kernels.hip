@@ -360,6 +360,20 @@ __device__ __forceinline__ RowSums across_wave(RowSums s) {
     return s;
 }
 
+// The sums of up to sixteen waves, every lane reading one of them.
+template <bool SQUARES>
+__device__ __forceinline__ RowSums across_16(const RowSums *sums, int waves) {
+    const int w = threadIdx.x & 15;
+    RowSums s = {0u, 0.0};
+    if (w < waves) s = sums[w];
+    for (int step = 1; step < 16; step <<= 1) {
+        RowSums o = {__shfl_xor(s.top, step), 0.0};
+        if (SQUARES) o.squares = __shfl_xor(s.squares, step);
+        s = join(s, o);
+    }
+    return s;
+}
+
 // e^(hi + lo) to about three roundings: the product with log2(e) keeps what it rounds off, since 2^p turns an absolute error of p into a
 // relative one.  Results below 2^-126 may be 0.
 __device__ __forceinline__ float exp_of(float hi, float lo) {
@@ -374,13 +388,13 @@ __device__ __forceinline__ float exp_of(float hi, float lo) {
 // the polynomial of degree 8 that a least-squares fit of the relative error at 400 Chebyshev points of t (a <= 15) gives: 3.6e-8 off, and 5 roundings in
 // all when evaluated in f32.  The form keeps its relative accuracy far out on the negative side, where 1 + erf has no digits left.
 template <int ACT>
-__device__ __forceinline__ float activate(float v) {
+__device__ __forceinline__ float activated(float v) {
     if constexpr (ACT == BNN_ACT_RELU) {
         return v > 0.0f || v != v ? v : 0.0f;
     } else if constexpr (ACT == BNN_ACT_SILU) {
         const float e = exp_of(-fminf(fabsf(v), 200.0f), 0.0f);
         return v * ((v < 0.0f ? e : 1.0f) * __builtin_amdgcn_rcpf(1.0f + e));
-    } else if constexpr (ACT == BNN_ACT_GELU) {
+    } else {
         const float a = fminf(fabsf(v), 20.0f), s = a * a;
         const float e = exp_of(-0.5f * s, -0.5f * fmaf(a, a, -s));
         const float t = __builtin_amdgcn_rcpf(fmaf(0.35f, a, 1.0f));
@@ -395,64 +409,87 @@ __device__ __forceinline__ float activate(float v) {
         r = fmaf(r, t, 0.13961990177631378f);
         const float phi = r * t * e;
         return v * (v < 0.0f ? phi : 1.0f - phi);
-    } else {
-        return v;
     }
 }
 
-// One row a workgroup of THREADS (a wave a row, four rows a workgroup, for THREADS = 64), its values in registers from the only
-// reading to the rounding: CHUNKS chunks of eight a thread.
+__device__ __forceinline__ void activate(int act, float (&v)[8]) {
+    if (act == BNN_ACT_SILU) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = activated<BNN_ACT_SILU>(v[j]);
+    } else if (act == BNN_ACT_GELU) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = activated<BNN_ACT_GELU>(v[j]);
+    } else if (act == BNN_ACT_RELU) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = activated<BNN_ACT_RELU>(v[j]);
+    }
+}
+
+// A row a workgroup of up to sixteen waves (SPREAD), or a row a wave, four of them in a workgroup; the row's values are in registers from the
+// only reading to the rounding, CHUNKS chunks of eight a thread.
 //   norm: v = h * weight; y = v / rms, a positive number for the whole row, so that q = 127 v / max|v| needs no rms and one
 //   reduction gives both the sum of squares and max|v|; only the scale, max|v| / (127 rms), takes it.
 //   gate: v = act(gate) * up.
-template <class T, bool NORM, int ACT, int THREADS, int CHUNKS>
-__global__ void __launch_bounds__(THREADS == 64 ? 256 : THREADS) rows_kernel(RowsClearArgs a) {
-    constexpr int kWaves = THREADS / 64, kRows = THREADS == 64 ? 4 : 1;
-    __shared__ RowSums sums[2][kWaves];
-    const int t = THREADS == 64 ? threadIdx.x & 63 : threadIdx.x;
+template <class T, bool NORM, bool SPREAD, int CHUNKS>
+__global__ void __launch_bounds__(!SPREAD ? 256 : CHUNKS <= 4 ? 1024 : 512) rows_kernel(RowsClearArgs a) {
+    __shared__ RowSums sums[2][16];
+    const int threads = SPREAD ? blockDim.x : 64, waves = threads >> 6, t = SPREAD ? threadIdx.x : threadIdx.x & 63;
+    const int64_t stride = SPREAD ? gridDim.x : (int64_t)gridDim.x * 4;
     int turn = 0;
-    for (int64_t row = (int64_t)blockIdx.x * kRows + (THREADS == 64 ? threadIdx.x >> 6 : 0); row < a.m;
-         row += (int64_t)gridDim.x * kRows, turn ^= 1) {
+    for (int64_t row = SPREAD ? blockIdx.x : (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); row < a.m; row += stride, turn ^= 1) {
         const T *pa = static_cast<const T *>(a.a) + row * a.lda, *pb = a.b ? static_cast<const T *>(a.b) + row * a.ldb : nullptr;
         float v[CHUNKS][8];
         RowSums s = {0u, 0.0};
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
-            const int at = 8 * (t + THREADS * c), left = a.k - at;
+            const int at = 8 * (t + threads * c), left = a.k - at;
+#pragma unroll
             for (int j = 0; j < 8; ++j) v[c][j] = 0.0f;
             if (left <= 0) continue;
-            float o[8];
             load_8(pa + at, left, v[c]);
+            if (NORM && a.b) {
+                float o[8];
+                load_8(pb + at, left, o);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[c][j] += o[j];
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) {
+            const int at = 8 * (t + threads * c), left = a.k - at;
+            // sixteen chunks fill the registers: four at a time, or the loads of all would be called for at once
+            if (CHUNKS > 8 && c % 4 == 0) __builtin_amdgcn_sched_barrier(0);
+            if (left <= 0) continue;
+            float o[8];
             if constexpr (NORM) {
-                if (a.b) {
-                    load_8(pb + at, left, o);
-                    for (int j = 0; j < 8; ++j) v[c][j] += o[j];
-                }
                 if (a.total) store_8(static_cast<T *>(a.total) + row * a.ldt + at, left, v[c]);
+#pragma unroll
                 for (int j = 0; j < 8; ++j) s.squares = fma((double)v[c][j], (double)v[c][j], s.squares);
                 if (a.weight) {
                     load_8(static_cast<const T *>(a.weight) + at, left, o);
+#pragma unroll
                     for (int j = 0; j < 8; ++j) v[c][j] *= o[j];
                 }
             } else {
-                for (int j = 0; j < 8; ++j) v[c][j] = activate<ACT>(v[c][j]);
-                if (a.b) {
-                    load_8(pb + at, left, o);
+                if (pb) load_8(pb + at, left, o);
+                activate(a.act, v[c]);
+                if (pb) {
+#pragma unroll
                     for (int j = 0; j < 8; ++j) v[c][j] *= o[j];
                 }
             }
+#pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const unsigned bits = __float_as_uint(v[c][j]) & 0x7fffffffu;
                 s.top = s.top > bits ? s.top : bits;
             }
         }
         s = across_wave<NORM>(s);
-        if constexpr (kWaves > 1) {
+        if (SPREAD && waves > 1) {
             // two places in turn: a wave that is a row ahead does not overwrite what another still reads
             if ((t & 63) == 0) sums[turn][t >> 6] = s;
             __syncthreads();
-            s = sums[turn][0];
-            for (int w = 1; w < kWaves; ++w) s = join(s, sums[turn][w]);
+            s = across_16<NORM>(sums[turn], waves);
         }
         const float top = __uint_as_float(s.top);
         if (t == 0) {
@@ -460,61 +497,92 @@ __global__ void __launch_bounds__(THREADS == 64 ? 256 : THREADS) rows_kernel(Row
             if (NORM) scale /= sqrt(s.squares / a.k + (double)a.eps);
             a.scale[row] = a.k ? (float)scale : 0.0f;
         }
-        // q = 127 v / top; rows near the bottom of the f32 range are lifted by 2^100 first, or 127 / top would be infinite
-        const float lift = top < 0x1p-100f ? 0x1p100f : 1.0f;
-        const float steps = s.top != 0u && s.top < 0x7f800000u ? 127.0f / (top * lift) : 0.0f;
+        // q = 127 v / top
+        float steps = 127.0f / top;
+        if (__builtin_expect(!(s.top >= 0x0d800000u && s.top < 0x7f800000u), 0)) {
+            if (s.top != 0u && s.top < 0x7f800000u) {
+                // near the bottom of the f32 range (below 2^-100) 127 / top would be infinite: lifted by 2^100 first
+                steps = 127.0f / (top * 0x1p100f);
+#pragma unroll
+                for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[c][j] *= 0x1p100f;
+            } else {
+                // nothing but zeros, or something that is not a number
+                steps = 0.0f;
+#pragma unroll
+                for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[c][j] = 0.0f;
+            }
+        }
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
-            const int at = 8 * (t + THREADS * c), left = a.k - at;
+            const int at = 8 * (t + threads * c), left = a.k - at;
             if (left <= 0) continue;
-            unsigned bytes[2] = {0u, 0u};
-            for (int j = 0; j < 8; ++j) {
-                // 1.5 * 2^23 added: the sum's last bits are the product rounded to the nearest whole number, once
-                float w = fmaf(v[c][j] * lift, steps, 12582912.0f);
-                if (steps == 0.0f) w = 12582912.0f;
-                bytes[j >> 2] |= (__float_as_uint(w) & 0xffu) << (8 * (j & 3));
+            unsigned bytes[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                // 1.5 * 2^23 added: the last byte of the sum is the product rounded to the nearest whole number, once
+                unsigned w[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) w[j] = __float_as_uint(fmaf(v[c][4 * h + j], steps, 12582912.0f));
+                bytes[h] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(w[3], w[2], 0x0c0c0400u), __builtin_amdgcn_perm(w[1], w[0], 0x0c0c0400u), 0x05040100u);
             }
             int8_t *q = a.q + row * a.ldq + at;
             if (left >= 8) {
                 __builtin_memcpy(q, bytes, 8);
             } else {
-                for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int j = 0; j < 7; ++j)
                     if (j < left) q[j] = (int8_t)(bytes[j >> 2] >> (8 * (j & 3)));
             }
         }
     }
 }
 
-template <class T, bool NORM, int ACT>
+// Threads and chunks a row.  Rows of up to 512 values: a wave each.  Longer ones: with fewer rows than
+// the device has CUs, as many threads as there are chunks, since then a row's time is the call's; otherwise about 256 threads with as many chunks
+// as it takes, so that several workgroups share a CU and each thread has several loads under way.
+template <class T, bool NORM>
 static void rows_launch(const RowsClearArgs &a, hipStream_t stream) {
-    const int64_t chunks = (a.k + 7) / 8;
-    if (chunks <= 64) rows_kernel<T, NORM, ACT, 64, 1><<<groups_of((a.m + 3) / 4), 256, 0, stream>>>(a);
-    else if (chunks <= 256) rows_kernel<T, NORM, ACT, 256, 1><<<groups_of(a.m), 256, 0, stream>>>(a);
-    else if (chunks <= 1024) rows_kernel<T, NORM, ACT, 1024, 1><<<groups_of(a.m), 1024, 0, stream>>>(a);
-    else if (chunks <= 2048) rows_kernel<T, NORM, ACT, 1024, 2><<<groups_of(a.m), 1024, 0, stream>>>(a);
-    else rows_kernel<T, NORM, ACT, 1024, 8><<<groups_of(a.m), 1024, 0, stream>>>(a);
+    const int chunks = (a.k + 7) / 8;
+    const auto ceil_div = [](int x, int y) { return (x + y - 1) / y; };
+    if (chunks <= 64) {
+        rows_kernel<T, NORM, false, 1><<<groups_of((a.m + 3) / 4), 256, 0, stream>>>(a);
+        return;
+    }
+    int each = ceil_div(chunks, a.m < 256 ? 1024 : 256);
+    // ROWS
+    if (each > 4 && chunks > 4096) each = 16;       // more than four chunks: up to 512 threads, which have the registers for them
+    each = each <= 1 ? 1 : each <= 2 ? 2 : each <= 3 ? 3 : each <= 4 ? 4 : each <= 6 ? 6 : each <= 8 ? 8 : 16;
+    const int threads = 64 * ceil_div(ceil_div(chunks, each), 64);
+    switch (each) {
+        case 1: rows_kernel<T, NORM, true, 1><<<groups_of(a.m), threads, 0, stream>>>(a); break;
+        case 2: rows_kernel<T, NORM, true, 2><<<groups_of(a.m), threads, 0, stream>>>(a); break;
+        case 3: rows_kernel<T, NORM, true, 3><<<groups_of(a.m), threads, 0, stream>>>(a); break;
+        case 4: rows_kernel<T, NORM, true, 4><<<groups_of(a.m), threads, 0, stream>>>(a); break;
+        case 6: rows_kernel<T, NORM, true, 6><<<groups_of(a.m), threads, 0, stream>>>(a); break;
+        case 8: rows_kernel<T, NORM, true, 8><<<groups_of(a.m), threads, 0, stream>>>(a); break;
+        default: rows_kernel<T, NORM, true, 16><<<groups_of(a.m), threads, 0, stream>>>(a); break;
+    }
 }
 
-template <bool NORM, int ACT>
+template <bool NORM>
 static void rows_typed(const RowsClearArgs &a, hipStream_t stream) {
-    if (a.type == BNN_CLEAR_F32) rows_launch<float, NORM, ACT>(a, stream);
-    else if (a.type == BNN_CLEAR_BF16) rows_launch<__hip_bfloat16, NORM, ACT>(a, stream);
-    else rows_launch<__half, NORM, ACT>(a, stream);
+    if (a.type == BNN_CLEAR_F32) rows_launch<float, NORM>(a, stream);
+    else if (a.type == BNN_CLEAR_BF16) rows_launch<__hip_bfloat16, NORM>(a, stream);
+    else rows_launch<__half, NORM>(a, stream);
 }
 
 int launch_norm_clear(const RowsClearArgs &a, hipStream_t stream) {
-    rows_typed<true, 0>(a, stream);
+    rows_typed<true>(a, stream);
     TFHE_HIP(hipGetLastError());
     return TFHE_OK;
 }
 
 int launch_gate_clear(const RowsClearArgs &a, hipStream_t stream) {
-    switch (a.act) {
-        case BNN_ACT_RELU: rows_typed<false, BNN_ACT_RELU>(a, stream); break;
-        case BNN_ACT_SILU: rows_typed<false, BNN_ACT_SILU>(a, stream); break;
-        case BNN_ACT_GELU: rows_typed<false, BNN_ACT_GELU>(a, stream); break;
-        default: rows_typed<false, BNN_ACT_IDENTITY>(a, stream); break;
-    }
+    rows_typed<false>(a, stream);
     TFHE_HIP(hipGetLastError());
     return TFHE_OK;
 }

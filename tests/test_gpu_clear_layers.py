@@ -515,12 +515,12 @@ def test_binding_refuses_what_does_not_fit(T):
         T.bnn_dense_clear(x, w, z(2, 4, t=torch.int32), x_scale=z(2, t=torch.float32))
     f, q, s = z(2, 8, t=torch.bfloat16), z(2, 8), z(2, t=torch.float32)
     for bad in (dict(weight=z(8, t=torch.float32)), dict(weight=z(7, t=torch.bfloat16)), dict(residual=z(2, 8, t=torch.half)), dict(total=z(2, 7, t=torch.bfloat16)),
-                dict(q=z(2, 8, t=torch.uint8)), dict(scale=z(2, t=torch.float64)), dict(scale=None)):
-        with pytest.raises((ValueError, T.TfheError)):
+                dict(q=z(2, 8, t=torch.uint8)), dict(scale=z(2, t=torch.float64))):
+        with pytest.raises(ValueError):
             T.bnn_rms_norm_clear(**dict(dict(x=f, weight=None, eps=1e-5, q=q, scale=s), **bad))
     with pytest.raises(T.TfheError):
         T.bnn_rms_norm_clear(q, None, 1e-5, q, s)
-    with pytest.raises((ValueError, KeyError)):
+    with pytest.raises(ValueError):
         T.bnn_gate_clear(f, None, "tanh", q, s)
     with pytest.raises(ValueError):
         T.bnn_gate_clear(f, z(2, 8, t=torch.float32), "silu", q, s)

@@ -31,8 +31,8 @@ struct RowsClearArgs {
 
 // largest k of a product: 128 * 128 * k stays below 2^31
 constexpr int64_t kMaxDenseClearK = 131071;
-// largest row of the norm and of the gate: 1,024 threads hold it in 64 registers each
-constexpr int64_t kMaxRowClear = 65536;
+// longest rows: 1,024 threads hold one in registers, the norm's 32 values each, the gate's 64
+constexpr int64_t kMaxNormClear = 32768, kMaxGateClear = 65536;
 
 int launch_dense_clear(const DenseClearArgs &a, hipStream_t stream);
 int launch_norm_clear(const RowsClearArgs &a, hipStream_t stream);

@@ -1,10 +1,7 @@
 // gfx950 kernels of layers in the clear: the 8-bit matrix product, and the two row operators that feed it (norm, gated activation).
 #include "clear_kernels.h"
 
-#include <type_traits>
-
-#include <hip/hip_bf16.h>
-#include <hip/hip_fp16.h>
+#include <algorithm>
 
 namespace tfhe {
 
@@ -75,13 +72,13 @@ __device__ __forceinline__ void finish_4(const DenseClearArgs &a, int64_t i, int
     if (a.kind == BNN_CLEAR_F32) {
         store_4(static_cast<float *>(a.out) + at, y, left);
     } else if (a.kind == BNN_CLEAR_BF16) {
-        __hip_bfloat16 o[4];
-        for (int e = 0; e < 4; ++e) o[e] = __float2bfloat16(y[e]);
-        store_4(static_cast<__hip_bfloat16 *>(a.out) + at, o, left);
+        __bf16 o[4];
+        for (int e = 0; e < 4; ++e) o[e] = (__bf16)y[e];
+        store_4(static_cast<__bf16 *>(a.out) + at, o, left);
     } else {
-        __half o[4];
-        for (int e = 0; e < 4; ++e) o[e] = __float2half(y[e]);
-        store_4(static_cast<__half *>(a.out) + at, o, left);
+        _Float16 o[4];
+        for (int e = 0; e < 4; ++e) o[e] = (_Float16)y[e];
+        store_4(static_cast<_Float16 *>(a.out) + at, o, left);
     }
 }
 
@@ -301,40 +298,62 @@ int launch_dense_clear(const DenseClearArgs &a, hipStream_t stream) {
 
 // ---- rows to 8 bits ------------------------------------------------------------------------------------------------
 
-// Eight neighbouring values of a row, `left` of which exist (those beyond are 0 and not touched).  The pointer is aligned to an
-// element only; the device takes wide accesses at any such address.
+// Eight neighbouring values as they lie in memory.
 template <class T>
 struct Eight {
     T v[8];
 };
 
-__device__ __forceinline__ float to_f32(float v) { return v; }
-__device__ __forceinline__ float to_f32(__hip_bfloat16 v) { return __bfloat162float(v); }
-__device__ __forceinline__ float to_f32(__half v) { return __half2float(v); }
-__device__ __forceinline__ void from_f32(float v, float &o) { o = v; }
-__device__ __forceinline__ void from_f32(float v, __hip_bfloat16 &o) { o = __float2bfloat16(v); }
-__device__ __forceinline__ void from_f32(float v, __half &o) { o = __float2half(v); }
+// A row is read in chunks of eight values.  Each thread reads CHUNKS of them, whole ones without a branch -- a chunk that is not
+// there is read at the row's beginning and replaced by zeros -- so that all its loads are under way at once; the one thread that
+// holds the row's last, partial chunk reads it value by value afterwards.  The pointer is aligned to a value only: the device takes wide
+// accesses at any such address.  The values are read once, past the caches' order of what to keep: 4096 x 10240 pairs in 34 us instead of 39.
+struct Chunks {
+    int t, threads, k;
+    __device__ __forceinline__ int at(int c) const { return 8 * (t + threads * c); }
+    __device__ __forceinline__ bool whole(int c) const { return at(c) + 8 <= k; }
+    __device__ __forceinline__ int partial(int c) const { return at(c) < k && !whole(c) ? k - at(c) : 0; }
+};
 
 template <class T>
-__device__ __forceinline__ void load_8(const T *p, int left, float (&out)[8]) {
-    if (left >= 8) {
-        Eight<T> e;
-        __builtin_memcpy(&e, p, sizeof e);
-        for (int j = 0; j < 8; ++j) out[j] = to_f32(e.v[j]);
-    } else {
-        for (int j = 0; j < 8; ++j) out[j] = j < left ? to_f32(p[j]) : 0.0f;
+__device__ __forceinline__ Eight<T> load_past(const T *p) {
+    typedef int Words __attribute__((ext_vector_type(sizeof(T) * 2), aligned(sizeof(T))));
+    const Words w = __builtin_nontemporal_load(reinterpret_cast<const Words *>(p));
+    Eight<T> e;
+    __builtin_memcpy(&e, &w, sizeof e);
+    return e;
+}
+
+template <class T, int COUNT>
+__device__ __forceinline__ void read_chunks(Eight<T> (&to)[COUNT], const T *row, const Chunks &own, int first) {
+#pragma unroll
+    for (int c = 0; c < COUNT; ++c) {
+        if (own.k >= 8) to[c] = load_past(row + (own.whole(first + c) ? own.at(first + c) : 0));
+        else __builtin_memset(&to[c], 0, sizeof to[c]);
+    }
+}
+
+// once the loads are under way: zeros for what is not there, the last values one by one
+template <class T>
+__device__ __forceinline__ void complete(Eight<T> &to, const T *row, const Chunks &own, int c) {
+    if (!own.whole(c)) {
+        __builtin_memset(&to, 0, sizeof to);
+        const int left = own.partial(c);
+#pragma unroll
+        for (int j = 0; j < 7; ++j)
+            if (j < left) to.v[j] = row[own.at(c) + j];
     }
 }
 
 template <class T>
-__device__ __forceinline__ void store_8(T *p, int left, const float (&in)[8]) {
-    if (left >= 8) {
-        Eight<T> e;
-        for (int j = 0; j < 8; ++j) from_f32(in[j], e.v[j]);
-        __builtin_memcpy(p, &e, sizeof e);
+__device__ __forceinline__ void write_8(T *row, const Eight<T> &e, const Chunks &own, int c) {
+    if (own.whole(c)) {
+        __builtin_memcpy(row + own.at(c), &e, sizeof e);
     } else {
-        for (int j = 0; j < 8; ++j)
-            if (j < left) from_f32(in[j], p[j]);
+        const int left = own.partial(c);
+#pragma unroll
+        for (int j = 0; j < 7; ++j)
+            if (j < left) row[own.at(c) + j] = e.v[j];
     }
 }
 
@@ -347,56 +366,68 @@ struct RowSums {
 };
 
 __device__ __forceinline__ RowSums join(RowSums a, RowSums b) {
-    return {a.top > b.top ? a.top : b.top, a.squares + b.squares};
+    return {std::max(a.top, b.top), a.squares + b.squares};
 }
 
+// The value that the lane `CTRL` says (a data-parallel-primitive control) holds; 0 where there is none.
+template <int CTRL>
+__device__ __forceinline__ unsigned from_lane(unsigned v) {
+    return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
+}
+
+template <int CTRL, bool SQUARES>
+__device__ __forceinline__ RowSums joined(RowSums s) {
+    RowSums o = {from_lane<CTRL>(s.top), 0.0};
+    if (SQUARES) {
+        const uint64_t bits = __double_as_longlong(s.squares);
+        o.squares = __longlong_as_double((uint64_t)from_lane<CTRL>((unsigned)(bits >> 32)) << 32 | from_lane<CTRL>((unsigned)bits));
+    }
+    return join(s, o);
+}
+
+// Over the wave, for every lane: sums of 2, 4, 8 and 16 neighbours by rotations within a row of 16 lanes, then across the four rows.
+// All in the vector unit: through LDS, as shuffles go, each of the six steps takes as long as this takes altogether.
 template <bool SQUARES>
 __device__ __forceinline__ RowSums across_wave(RowSums s) {
-    for (int step = 1; step < 64; step <<= 1) {
-        RowSums o = {__shfl_xor(s.top, step), 0.0};
-        if (SQUARES) o.squares = __shfl_xor(s.squares, step);
-        s = join(s, o);
+    s = joined<0x121, SQUARES>(s);      // row_ror:1, 2, 4, 8
+    s = joined<0x122, SQUARES>(s);
+    s = joined<0x124, SQUARES>(s);
+    s = joined<0x128, SQUARES>(s);
+    RowSums all = {0u, 0.0};
+#pragma unroll
+    for (int row = 0; row < 4; ++row) {
+        RowSums o = {(unsigned)__builtin_amdgcn_readlane((int)s.top, 16 * row), 0.0};
+        if (SQUARES) {
+            const uint64_t bits = __double_as_longlong(s.squares);
+            o.squares = __longlong_as_double((uint64_t)(unsigned)__builtin_amdgcn_readlane((int)(bits >> 32), 16 * row) << 32 |
+                                             (unsigned)__builtin_amdgcn_readlane((int)bits, 16 * row));
+        }
+        all = row ? join(all, o) : o;
     }
-    return s;
+    return all;
 }
 
-// The sums of up to sixteen waves, every lane reading one of them.
-template <bool SQUARES>
-__device__ __forceinline__ RowSums across_16(const RowSums *sums, int waves) {
-    const int w = threadIdx.x & 15;
-    RowSums s = {0u, 0.0};
-    if (w < waves) s = sums[w];
-    for (int step = 1; step < 16; step <<= 1) {
-        RowSums o = {__shfl_xor(s.top, step), 0.0};
-        if (SQUARES) o.squares = __shfl_xor(s.squares, step);
-        s = join(s, o);
-    }
-    return s;
-}
-
-// e^(hi + lo) to about three roundings: the product with log2(e) keeps what it rounds off, since 2^p turns an absolute error of p into a
-// relative one.  Results below 2^-126 may be 0.
-__device__ __forceinline__ float exp_of(float hi, float lo) {
-    constexpr float kLog2e = 1.44269502f, kRest = 1.92596303e-8f, kLn2 = 0.693147182f;
-    const float p = hi * kLog2e;
-    const float r = fmaf(hi, kLog2e, -p) + fmaf(hi, kRest, lo * kLog2e);
-    return __builtin_amdgcn_exp2f(p) * fmaf(r, kLn2, 1.0f);
-}
-
-// silu(v) = v / (1 + e^-v), from e^-|v| so that nothing overflows.
-// gelu(v) = v Phi(v).  Phi(-a) = e^(-a^2/2) R(a) for a >= 0, R the scaled complementary error function; R as t P(t), t = 1 / (1 + 0.35 a), P
-// the polynomial of degree 8 that a least-squares fit of the relative error at 400 Chebyshev points of t (a <= 15) gives: 3.6e-8 off, and 5 roundings in
-// all when evaluated in f32.  The form keeps its relative accuracy far out on the negative side, where 1 + erf has no digits left.
+// relu; silu(v) = v / (1 + e^-v); gelu(v) = v Phi(v).  With up to 4096 x 10240 values a prompt these are bound by their instructions as much as by
+// memory, so both are as short as their accuracy allows:
+//   silu: e^-v as 2^p, the product p = -v log2(e) with what it rounds off, since 2^p turns an absolute error of p into a relative one:
+//   about eight roundings at any v.  What is below 2^-119 may be 0.
+//   gelu: Phi(-a) = e^(-a^2/2) R(a) for a >= 0, R the scaled complementary error function; R as t P(t), t = 1 / (1 + 0.35 a), P
+//   the polynomial of degree 8 that a least-squares fit of the relative error at 400 Chebyshev points of t (a <= 15) gives: 3.6e-8 off, and 5
+//   roundings when evaluated in f32.  v Phi(v) is then max(v, 0) - |v| Phi(-|v|).  This keeps its relative accuracy far out on the negative
+//   side, where 1 + erf has no digits left; there the rounding of a^2 grows to 1.5 a^2 roundings of the result.
 template <int ACT>
 __device__ __forceinline__ float activated(float v) {
     if constexpr (ACT == BNN_ACT_RELU) {
         return v > 0.0f || v != v ? v : 0.0f;
     } else if constexpr (ACT == BNN_ACT_SILU) {
-        const float e = exp_of(-fminf(fabsf(v), 200.0f), 0.0f);
-        return v * ((v < 0.0f ? e : 1.0f) * __builtin_amdgcn_rcpf(1.0f + e));
+        constexpr float kLog2e = 1.44269502f, kRest = 1.92596303e-8f, kLn2 = 0.693147182f;
+        const float h = __builtin_amdgcn_fmed3f(-v, -200.0f, 200.0f), p = h * kLog2e;
+        const float r = fmaf(h, kRest, fmaf(h, kLog2e, -p));
+        const float e = __builtin_amdgcn_exp2f(p) * fmaf(r, kLn2, 1.0f);
+        return v * __builtin_amdgcn_rcpf(1.0f + e);
     } else {
-        const float a = fminf(fabsf(v), 20.0f), s = a * a;
-        const float e = exp_of(-0.5f * s, -0.5f * fmaf(a, a, -s));
+        const float a = fminf(fabsf(v), 20.0f);
+        const float e = __builtin_amdgcn_exp2f(a * a * -0.72134752f);
         const float t = __builtin_amdgcn_rcpf(fmaf(0.35f, a, 1.0f));
         float r = -0.02949463576078415f;
         r = fmaf(r, t, 0.14561739563941956f);
@@ -407,8 +438,7 @@ __device__ __forceinline__ float activated(float v) {
         r = fmaf(r, t, 0.11960979551076889f);
         r = fmaf(r, t, 0.1398903727531433f);
         r = fmaf(r, t, 0.13961990177631378f);
-        const float phi = r * t * e;
-        return v * (v < 0.0f ? phi : 1.0f - phi);
+        return fmaf(-fabsf(v), r * t * e, fmaxf(v, 0.0f));
     }
 }
 
@@ -431,73 +461,77 @@ __device__ __forceinline__ void activate(int act, float (&v)[8]) {
 //   reduction gives both the sum of squares and max|v|; only the scale, max|v| / (127 rms), takes it.
 //   gate: v = act(gate) * up.
 template <class T, bool NORM, bool SPREAD, int CHUNKS>
-__global__ void __launch_bounds__(!SPREAD ? 256 : CHUNKS <= 4 ? 1024 : 512) rows_kernel(RowsClearArgs a) {
+__global__ void __launch_bounds__(SPREAD ? 1024 : 256) rows_kernel(RowsClearArgs a) {
     __shared__ RowSums sums[2][16];
-    const int threads = SPREAD ? blockDim.x : 64, waves = threads >> 6, t = SPREAD ? threadIdx.x : threadIdx.x & 63;
+    const int threads = SPREAD ? blockDim.x : 64, waves = threads >> 6;
+    Chunks own = {SPREAD ? (int)threadIdx.x : (int)(threadIdx.x & 63), threads, a.k};
     const int64_t stride = SPREAD ? gridDim.x : (int64_t)gridDim.x * 4;
     int turn = 0;
-    for (int64_t row = SPREAD ? blockIdx.x : (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); row < a.m; row += stride, turn ^= 1) {
+    for (int64_t row = SPREAD ? blockIdx.x : (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); row < a.m;
+         row += stride, turn ^= 1) {
+        // what goes by the thread is found anew for each row: kept from row to row, the many addresses and conditions of more than two chunks
+        // crowd values out of the registers
+        asm volatile("" : "+v"(own.t));
         const T *pa = static_cast<const T *>(a.a) + row * a.lda, *pb = a.b ? static_cast<const T *>(a.b) + row * a.ldb : nullptr;
+        const T *weight = static_cast<const T *>(a.weight);
+        constexpr int kTogether = CHUNKS == 1 ? 1 : 2;     // chunks whose loads are under way at once, as registers allow
+        Eight<T> ra[kTogether], rb[kTogether];
         float v[CHUNKS][8];
         RowSums s = {0u, 0.0};
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
-            const int at = 8 * (t + threads * c), left = a.k - at;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[c][j] = 0.0f;
-            if (left <= 0) continue;
-            load_8(pa + at, left, v[c]);
-            if (NORM && a.b) {
-                float o[8];
-                load_8(pb + at, left, o);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[c][j] += o[j];
+            if (CHUNKS > kTogether) __builtin_amdgcn_sched_barrier(0);
+            if (c % kTogether == 0) {
+                read_chunks(ra, pa, own, c);
+                if (pb) read_chunks(rb, pb, own, c);
             }
-        }
+            complete(ra[c % kTogether], pa, own, c);
+            if (pb) complete(rb[c % kTogether], pb, own, c);
 #pragma unroll
-        for (int c = 0; c < CHUNKS; ++c) {
-            const int at = 8 * (t + threads * c), left = a.k - at;
-            // sixteen chunks fill the registers: four at a time, or the loads of all would be called for at once
-            if (CHUNKS > 8 && c % 4 == 0) __builtin_amdgcn_sched_barrier(0);
-            if (left <= 0) continue;
-            float o[8];
+            for (int j = 0; j < 8; ++j) v[c][j] = (float)ra[c % kTogether].v[j];
             if constexpr (NORM) {
-                if (a.total) store_8(static_cast<T *>(a.total) + row * a.ldt + at, left, v[c]);
+                if (pb) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[c][j] += (float)rb[c % kTogether].v[j];
+                }
+                if (a.total) {
+                    Eight<T> h;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) h.v[j] = (T)v[c][j];
+                    write_8(static_cast<T *>(a.total) + row * a.ldt, h, own, c);
+                }
 #pragma unroll
                 for (int j = 0; j < 8; ++j) s.squares = fma((double)v[c][j], (double)v[c][j], s.squares);
-                if (a.weight) {
-                    load_8(static_cast<const T *>(a.weight) + at, left, o);
+                if (weight) {
+                    Eight<T> g;
+                    if (own.whole(c)) __builtin_memcpy(&g, weight + own.at(c), sizeof g);
+                    complete(g, weight, own, c);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) v[c][j] *= o[j];
+                    for (int j = 0; j < 8; ++j) v[c][j] *= (float)g.v[j];
                 }
             } else {
-                if (pb) load_8(pb + at, left, o);
                 activate(a.act, v[c]);
                 if (pb) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) v[c][j] *= o[j];
+                    for (int j = 0; j < 8; ++j) v[c][j] *= (float)rb[c % kTogether].v[j];
                 }
             }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const unsigned bits = __float_as_uint(v[c][j]) & 0x7fffffffu;
-                s.top = s.top > bits ? s.top : bits;
+            for (int j = 0; j < 8; j += 2) {
+                const unsigned x = __float_as_uint(v[c][j]) & 0x7fffffffu, y = __float_as_uint(v[c][j + 1]) & 0x7fffffffu;
+                s.top = std::max(s.top, std::max(x, y));
             }
         }
         s = across_wave<NORM>(s);
         if (SPREAD && waves > 1) {
             // two places in turn: a wave that is a row ahead does not overwrite what another still reads
-            if ((t & 63) == 0) sums[turn][t >> 6] = s;
+            if ((threadIdx.x & 63) == 0) sums[turn][threadIdx.x >> 6] = s;
             __syncthreads();
-            s = across_16<NORM>(sums[turn], waves);
-        }
-        const float top = __uint_as_float(s.top);
-        if (t == 0) {
-            double scale = (double)top / 127.0;
-            if (NORM) scale /= sqrt(s.squares / a.k + (double)a.eps);
-            a.scale[row] = a.k ? (float)scale : 0.0f;
+            s = sums[turn][0];
+            for (int w = 1; w < waves; ++w) s = join(s, sums[turn][w]);
         }
         // q = 127 v / top
+        const float top = __uint_as_float(s.top);
         float steps = 127.0f / top;
         if (__builtin_expect(!(s.top >= 0x0d800000u && s.top < 0x7f800000u), 0)) {
             if (s.top != 0u && s.top < 0x7f800000u) {
@@ -518,8 +552,6 @@ __global__ void __launch_bounds__(!SPREAD ? 256 : CHUNKS <= 4 ? 1024 : 512) rows
         }
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
-            const int at = 8 * (t + threads * c), left = a.k - at;
-            if (left <= 0) continue;
             unsigned bytes[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -529,50 +561,48 @@ __global__ void __launch_bounds__(!SPREAD ? 256 : CHUNKS <= 4 ? 1024 : 512) rows
                 for (int j = 0; j < 4; ++j) w[j] = __float_as_uint(fmaf(v[c][4 * h + j], steps, 12582912.0f));
                 bytes[h] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(w[3], w[2], 0x0c0c0400u), __builtin_amdgcn_perm(w[1], w[0], 0x0c0c0400u), 0x05040100u);
             }
-            int8_t *q = a.q + row * a.ldq + at;
-            if (left >= 8) {
-                __builtin_memcpy(q, bytes, 8);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 7; ++j)
-                    if (j < left) q[j] = (int8_t)(bytes[j >> 2] >> (8 * (j & 3)));
-            }
+            Eight<int8_t> q;
+            __builtin_memcpy(&q, bytes, sizeof q);
+            write_8(a.q + row * a.ldq, q, own, c);
+        }
+        if (own.t == 0) {
+            double scale = (double)top / 127.0;
+            if (NORM) scale /= sqrt(s.squares / a.k + (double)a.eps);
+            a.scale[row] = a.k ? (float)scale : 0.0f;
         }
     }
 }
 
-// Threads and chunks a row.  Rows of up to 512 values: a wave each.  Longer ones: with fewer rows than
-// the device has CUs, as many threads as there are chunks, since then a row's time is the call's; otherwise about 256 threads with as many chunks
-// as it takes, so that several workgroups share a CU and each thread has several loads under way.
+// Threads and chunks a row.  Up to 512 values: a wave a row, and no workgroup to meet.  Longer rows: a thread a chunk as long as rows
+// are few or short, since a row's time is then the call's (300 x 4096 gate 4.4 us, two chunks a thread 5.0); else the fewest threads that keep
+// enough waves on a CU, two chunks each, four from 1,024 chunks on (8192 x 8192 bf16 norm, one, two, four chunks a thread: 129, 90, 100 us; 4096 x 14336 silu,
+// two, four, six: 72, 61, 82).  The norm's weights and second output take it registers: with four its waves no longer fit (2048 x 12288 bf16, two, four: 37, 51).
+// Rows of more than 16,384 values have no choice.
 template <class T, bool NORM>
 static void rows_launch(const RowsClearArgs &a, hipStream_t stream) {
     const int chunks = (a.k + 7) / 8;
-    const auto ceil_div = [](int x, int y) { return (x + y - 1) / y; };
     if (chunks <= 64) {
         rows_kernel<T, NORM, false, 1><<<groups_of((a.m + 3) / 4), 256, 0, stream>>>(a);
         return;
     }
-    int each = ceil_div(chunks, a.m < 256 ? 1024 : 256);
+    int each = chunks <= 256 || (chunks <= 512 && a.m < 1024) ? 1 : chunks <= 1024 ? 2 : chunks <= 2048 ? (NORM || a.m < 512 ? 2 : 4) : chunks <= 4096 ? 4 : 8;
     // ROWS
-    if (each > 4 && chunks > 4096) each = 16;       // more than four chunks: up to 512 threads, which have the registers for them
-    each = each <= 1 ? 1 : each <= 2 ? 2 : each <= 3 ? 3 : each <= 4 ? 4 : each <= 6 ? 6 : each <= 8 ? 8 : 16;
-    const int threads = 64 * ceil_div(ceil_div(chunks, each), 64);
+    const int threads = 64 * (((chunks + each - 1) / each + 63) / 64);
     switch (each) {
         case 1: rows_kernel<T, NORM, true, 1><<<groups_of(a.m), threads, 0, stream>>>(a); break;
         case 2: rows_kernel<T, NORM, true, 2><<<groups_of(a.m), threads, 0, stream>>>(a); break;
-        case 3: rows_kernel<T, NORM, true, 3><<<groups_of(a.m), threads, 0, stream>>>(a); break;
         case 4: rows_kernel<T, NORM, true, 4><<<groups_of(a.m), threads, 0, stream>>>(a); break;
-        case 6: rows_kernel<T, NORM, true, 6><<<groups_of(a.m), threads, 0, stream>>>(a); break;
-        case 8: rows_kernel<T, NORM, true, 8><<<groups_of(a.m), threads, 0, stream>>>(a); break;
-        default: rows_kernel<T, NORM, true, 16><<<groups_of(a.m), threads, 0, stream>>>(a); break;
+        default:
+            if constexpr (!NORM) rows_kernel<T, NORM, true, 8><<<groups_of(a.m), threads, 0, stream>>>(a);
+            break;
     }
 }
 
 template <bool NORM>
 static void rows_typed(const RowsClearArgs &a, hipStream_t stream) {
     if (a.type == BNN_CLEAR_F32) rows_launch<float, NORM>(a, stream);
-    else if (a.type == BNN_CLEAR_BF16) rows_launch<__hip_bfloat16, NORM>(a, stream);
-    else rows_launch<__half, NORM>(a, stream);
+    else if (a.type == BNN_CLEAR_BF16) rows_launch<__bf16, NORM>(a, stream);
+    else rows_launch<_Float16, NORM>(a, stream);
 }
 
 int launch_norm_clear(const RowsClearArgs &a, hipStream_t stream) {

@@ -53,14 +53,14 @@ static int dense_clear(const DenseClearArgs &a, int64_t k, void *stream) {
     return launch_dense_clear(a, static_cast<hipStream_t>(stream));
 }
 
-static int check_8bit_rows(const RowsClearArgs &a, int64_t k) {
+static int check_8bit_rows(const RowsClearArgs &a, int64_t k, int64_t most) {
     if (a.type < BNN_CLEAR_F32 || a.type > BNN_CLEAR_F16) return set_error(TFHE_E_PARAM, "unknown input type %d", a.type);
-    if (int rc = check_rows(a.m, k, kMaxRowClear)) return rc;
+    if (int rc = check_rows(a.m, k, most)) return rc;
     return check_stride("q", a.ldq, k);
 }
 
 static int norm_clear(const RowsClearArgs &a, int64_t k, void *stream) {
-    if (int rc = check_8bit_rows(a, k)) return rc;
+    if (int rc = check_8bit_rows(a, k, kMaxNormClear)) return rc;
     if (!(a.eps > 0) || !(a.eps < INFINITY)) return set_error(TFHE_E_PARAM, "eps must be positive and finite");
     if (int rc = check_stride("x", a.lda, k)) return rc;
     if (a.b)
@@ -80,7 +80,7 @@ static int norm_clear(const RowsClearArgs &a, int64_t k, void *stream) {
 }
 
 static int gate_clear(const RowsClearArgs &a, int64_t k, void *stream) {
-    if (int rc = check_8bit_rows(a, k)) return rc;
+    if (int rc = check_8bit_rows(a, k, kMaxGateClear)) return rc;
     if (a.act < BNN_ACT_IDENTITY || a.act > BNN_ACT_GELU) return set_error(TFHE_E_PARAM, "unknown activation %d", a.act);
     if (int rc = check_stride("gate", a.lda, k)) return rc;
     if (a.b)

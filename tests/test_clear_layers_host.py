@@ -43,7 +43,7 @@ def test_product_refusals(change, code, word):
     (dict(type=3), PARAM, "type"), (dict(type=-1), PARAM, "type"),
     (dict(eps=0.0), PARAM, "eps"), (dict(eps=-1.0), PARAM, "eps"), (dict(eps=math.inf), PARAM, "eps"), (dict(eps=math.nan), PARAM, "eps"),
     (dict(m=-1), SIZE, "rows"), (dict(k=-1), SIZE, "rows"), (dict(m=2**31), SIZE, "rows"),
-    (dict(k=65537, ldx=65537, ldr=65537, ldt=65537, ldq=65537), SIZE, "at most 65536"),
+    (dict(k=32769, ldx=32769, ldr=32769, ldt=32769, ldq=32769), SIZE, "at most 32768"),
     (dict(ldx=63), SIZE, "stride"), (dict(ldr=63), SIZE, "stride"), (dict(ldt=63), SIZE, "stride"), (dict(ldq=63), SIZE, "stride"),
     (dict(x=None), NULL, "x"), (dict(q=None), NULL, "q"), (dict(scale=None), NULL, "scale"),
     (dict(x=P + 1), PARAM, "aligned"), (dict(residual=P + 1), PARAM, "aligned"), (dict(weight=P + 1), PARAM, "aligned"),

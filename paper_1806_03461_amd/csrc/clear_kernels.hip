@@ -2,11 +2,11 @@
 #include "clear_kernels.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace tfhe {
 
 typedef int v4i __attribute__((ext_vector_type(4)));
-typedef int v16i __attribute__((ext_vector_type(16)));
 
 // ---- the product ---------------------------------------------------------------------------------------------------
 
@@ -45,160 +45,277 @@ __device__ __forceinline__ void store_4(T *p, const T (&v)[4], int left) {
     }
 }
 
-// The outputs of four neighbouring channels of token i, j .. j + 3, of which those below n exist, from their sums.
-__device__ __forceinline__ void finish_4(const DenseClearArgs &a, int64_t i, int64_t j, v4i acc) {
-    const int left = a.n - j < 4 ? (int)(a.n - j) : 4;
+// What four neighbouring channels j .. j + 3, of which `left` exist, bring to their outputs.
+struct Channels {
+    float scale[4];
+    int bias[4];        // bits of the floats or the whole numbers that they are
+    int left;
+};
+
+// The outputs of token i and channels j .. j + 3 from their sums.
+__device__ __forceinline__ void finish_4(const DenseClearArgs &a, int64_t i, int64_t j, v4i acc, float x_scale, const Channels &c) {
     const int64_t at = i * a.ldo + j;
     if (a.kind >= BNN_CLEAR_I32) {
-        int b[4] = {0, 0, 0, 0};
-        if (a.bias) load_4(b, static_cast<const int *>(a.bias) + j, left);
         if (a.kind == BNN_CLEAR_I32) {
             int o[4];
-            for (int e = 0; e < 4; ++e) o[e] = (int)((unsigned)acc[e] + (unsigned)b[e]);
-            store_4(static_cast<int *>(a.out) + at, o, left);
+            for (int e = 0; e < 4; ++e) o[e] = (int)((unsigned)acc[e] + (unsigned)c.bias[e]);
+            store_4(static_cast<int *>(a.out) + at, o, c.left);
         } else {
             const int8_t no = a.kind == BNN_CLEAR_SIGN ? -1 : 0;
             int8_t o[4];
-            for (int e = 0; e < 4; ++e) o[e] = (int64_t)acc[e] + b[e] >= 0 ? (int8_t)1 : no;
-            store_4(static_cast<int8_t *>(a.out) + at, o, left);
+            for (int e = 0; e < 4; ++e) o[e] = (int64_t)acc[e] + c.bias[e] >= 0 ? (int8_t)1 : no;
+            store_4(static_cast<int8_t *>(a.out) + at, o, c.left);
         }
         return;
     }
-    float sw[4] = {1.0f, 1.0f, 1.0f, 1.0f}, b[4] = {0.0f, 0.0f, 0.0f, 0.0f}, y[4];
-    const float sx = a.x_scale ? a.x_scale[i] : 1.0f;
-    if (a.w_scale) load_4(sw, a.w_scale + j, left);
-    if (a.bias) load_4(b, static_cast<const float *>(a.bias) + j, left);
-    for (int e = 0; e < 4; ++e) y[e] = (float)acc[e] * sx * sw[e] + b[e];
+    float y[4];
+    for (int e = 0; e < 4; ++e) y[e] = (float)acc[e] * x_scale * c.scale[e] + __int_as_float(c.bias[e]);
     if (a.kind == BNN_CLEAR_F32) {
-        store_4(static_cast<float *>(a.out) + at, y, left);
+        store_4(static_cast<float *>(a.out) + at, y, c.left);
     } else if (a.kind == BNN_CLEAR_BF16) {
         __bf16 o[4];
         for (int e = 0; e < 4; ++e) o[e] = (__bf16)y[e];
-        store_4(static_cast<__bf16 *>(a.out) + at, o, left);
+        store_4(static_cast<__bf16 *>(a.out) + at, o, c.left);
     } else {
         _Float16 o[4];
         for (int e = 0; e < 4; ++e) o[e] = (_Float16)y[e];
-        store_4(static_cast<_Float16 *>(a.out) + at, o, left);
+        store_4(static_cast<_Float16 *>(a.out) + at, o, c.left);
     }
 }
 
-// Waits until at most `left` of the wave's loads into LDS are under way and its reads of LDS have come, then meets the workgroup.
+// Waits until at most `left` of the wave's loads into LDS are under way, then meets the workgroup.
 template <int left>
 __device__ __forceinline__ void landed_and_meet() {
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(left) : "memory");
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(left) : "memory");
 }
 
-// Tiles of (WT * RT * 32) tokens by (WC * RC * 32) channels, a workgroup of WT x WC waves each, every wave RT x RC products of 32 by 32.
-// 128 bytes of k at a time go through LDS, the next 128 under way while these are multiplied.  A row's eight 16-byte pieces lie in
-// LDS at place (piece ^ row % 8), so that the eight lanes that read one piece of eight rows meet all banks.
+// The same with all loads, and all of the wave's reads and writes of LDS.
+__device__ __forceinline__ void settled_and_meet() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// Memory that buffer loads see: `bytes` from p on.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const int8_t *p, int bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t *>(p), (short)0, bytes, 0x00020000);
+}
+
+// 16 bytes a lane from memory into LDS: lane l's go to `to` + 16 l.
+__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t from, int offset, int step, int8_t *to) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void *)to, 16, offset, step, 0, 0);
+}
+
+// Tiles of (WT * RT * 16) tokens by (WC * RC * 16) channels, a workgroup of WT x WC waves each, every wave RT x RC products of 16 by 16.
+// (Products of 32 by 32 do the same work with half the instructions, but read and write every sum twice as often: on all CUs and random operands,
+// where power sets the clock, 3.2 Pop/s of them against 3.9 of these.)
+// BK bytes of k are a step, and four steps have a place in LDS: the wave holds one step's operands in registers and reads the
+// next one's behind each row of products, and the loads of the two after that are under way.  The places are four arrays and the loop is unrolled over
+// them, or the compiler would take each read of LDS to depend on the loads into it and wait for them all.  A row's 16-byte pieces lie in LDS at place (piece ^
+// something of the row), so that eight lanes that read the same piece of eight rows meet all banks.
 // The channels are the products' rows: a lane then holds four neighbouring channels of a token.
-//   ALIGNED: rows begin at multiples of 16 bytes and k is one too; pieces go from memory to LDS directly.  Otherwise through registers.
-template <int WT, int WC, int RT, int RC, bool ALIGNED>
-__global__ void __launch_bounds__(64 * WT * WC, 2) dense_tile_kernel(DenseClearArgs a) {
-    constexpr int kThreads = 64 * WT * WC, kWaves = WT * WC, TT = 32 * WT * RT, TC = 32 * WC * RC;
-    constexpr int kPieces = (TT + TC) * 8 / kThreads;       // of 16 bytes, a thread
-    constexpr int kXPieces = TT * 8 / kThreads;
-    constexpr int kRow = 32 * RC + 4;                       // words of a token's channels as the sums pass through LDS
-    static_assert(kWaves * 32 * kRow * 4 <= 2 * (TT + TC) * 128, "the sums pass through the operands' LDS");
-    static_assert(kXPieces * kThreads == TT * 8 && kPieces * kThreads == (TT + TC) * 8, "whole pieces a thread");
-    __shared__ __attribute__((aligned(1024))) int8_t lds[2][(TT + TC) * 128];
+//   DIRECT: rows begin at multiples of 4 bytes, and pieces go from memory to LDS directly, but for the last step if k is no whole number of
+//   steps.  Otherwise all go through registers, two steps ahead.
+template <int WT, int WC, int RT, int RC, int BK, bool DIRECT>
+__global__ void __launch_bounds__(64 * WT * WC, RT * RC == 64 ? 1 : 2) dense_tile_kernel(DenseClearArgs a) {
+    constexpr int kThreads = 64 * WT * WC, kWaves = WT * WC, TT = 16 * WT * RT, TC = 16 * WC * RC;
+    constexpr int kPerRow = BK / 16;                        // pieces a row
+    constexpr int kRows = kThreads / kPerRow;               // rows of one piece a thread
+    constexpr int kXPieces = TT / kRows, kPieces = (TT + TC) / kRows;
+    constexpr int kStage = (TT + TC) * BK, kInner = BK / 64;
+    constexpr int kRow = 16 * RC + 4;                       // words of a token's channels as its sums pass through LDS
+    static_assert(kXPieces * kRows == TT && kPieces * kRows == TT + TC && kRows % 8 == 0, "whole pieces a thread");
+    constexpr int kPerPlace = (kWaves + 3) / 4;             // waves whose sums pass through one place
+    static_assert(kPerPlace * 32 * kRow * 4 <= kStage, "the sums pass through the operands' LDS");
+    __shared__ __attribute__((aligned(1024))) int8_t place_0[kStage], place_1[kStage], place_2[kStage], place_3[kStage];
+    int8_t *const place[4] = {place_0, place_1, place_2, place_3};
+    __shared__ __attribute__((aligned(16))) float x_scales[TT], w_scales[TC];
+    __shared__ __attribute__((aligned(16))) int biases[TC];
+    static_assert(TT <= kThreads && TC <= kThreads, "a thread a token or channel");
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
-    const int64_t across = (a.n + TC - 1) / TC, down = (a.m + TT - 1) / TT, tiles = across * down;
-    const int steps = (a.k + 127) / 128;
-    for (int64_t id = blockIdx.x; id < tiles; id += gridDim.x) {
+    const unsigned across = (unsigned)((a.n + TC - 1) / TC), down = (unsigned)((a.m + TT - 1) / TT), tiles = across * down;
+    const int whole = a.k / BK, steps = (a.k + BK - 1) / BK;
+    const auto turned = [](int row) { return BK == 128 ? row & 7 : (row >> 1) & 3; };
+    for (unsigned id = blockIdx.x; id < tiles; id += gridDim.x) {
         // Workgroups go round the eight XCDs; each XCD gets neighbouring tiles, four token tiles by all channels at a time, so that
         // its L2 is asked for the same rows.
-        const int64_t xcd = id & 7, share = tiles >> 3, over = tiles & 7;
-        const int64_t lin = xcd * share + (xcd < over ? xcd : over) + (id >> 3);
-        const int64_t band = lin / (4 * across), in_band = lin - band * 4 * across, first = band * 4, high = down - first < 4 ? down - first : 4;
-        const int64_t i0 = (first + in_band % high) * TT, j0 = in_band / high * TC;
+        const unsigned xcd = id & 7, share = tiles >> 3, over = tiles & 7, lin = xcd * share + std::min(xcd, over) + (id >> 3);
+        const unsigned band = lin / (4 * across), in_band = lin - band * 4 * across, first = band * 4, high = std::min(down - first, 4u);
+        const int64_t i0 = (int64_t)(first + in_band % high) * TT, j0 = (int64_t)(in_band / high) * TC;
 
-        // piece p of a thread: row p * kThreads / 8 + t / 8 of the tile's tokens, then of its channels
-        const int place = t & 7, row8 = t >> 3, piece = place ^ (row8 & 7);
-        const int8_t *row[kPieces];
+        // what the outputs take, asked for now and laid aside before the first product
+        const bool x_mine = t < TT && i0 + t < a.m, w_mine = t < TC && j0 + t < a.n;
+        const float my_x_scale = x_mine && a.x_scale ? a.x_scale[i0 + t] : 1.0f, my_w_scale = w_mine && a.w_scale ? a.w_scale[j0 + t] : 1.0f;
+        const int my_bias = w_mine && a.bias ? static_cast<const int *>(a.bias)[j0 + t] : 0;
+        // piece p of a thread: row p * kRows + t / kPerRow of the tile's tokens, then of its channels
+        const int my_row = t / kPerRow, piece = t % kPerRow ^ turned(my_row);
+        int64_t row[kPieces];
         int offset[kPieces];
 #pragma unroll
         for (int p = 0; p < kPieces; ++p) {
             const bool is_x = p < kXPieces;
-            const int64_t r = (is_x ? i0 : j0) + (p - (is_x ? 0 : kXPieces)) * (kThreads / 8) + row8, rows = is_x ? a.m : a.n;
+            const int64_t r = (is_x ? i0 : j0) + (p - (is_x ? 0 : kXPieces)) * kRows + my_row, rows = is_x ? a.m : a.n;
             const int64_t kept = r < rows ? r : rows - 1;       // beyond the last row: that row again, never stored
-            if (ALIGNED) offset[p] = (int)((kept - (is_x ? i0 : j0)) * (is_x ? a.ldx : a.ldw)) + 16 * piece;
-            else row[p] = is_x ? a.x + kept * a.ldx : a.w + kept * a.ldw;
+            row[p] = kept * (is_x ? a.ldx : a.ldw);
+            if (DIRECT) offset[p] = (int)(row[p] - (is_x ? i0 * a.ldx : j0 * a.ldw)) + 16 * piece;
         }
-        const int64_t x_end = ((a.m - i0 < TT ? a.m - i0 : TT) - 1) * a.ldx + a.k, w_end = ((a.n - j0 < TC ? a.n - j0 : TC) - 1) * a.ldw + a.k;
-        const auto xr = __builtin_amdgcn_make_buffer_rsrc((void *)(a.x + i0 * a.ldx), (short)0, (int)x_end, 0x00020000);
-        const auto wr = __builtin_amdgcn_make_buffer_rsrc((void *)(a.w + j0 * a.ldw), (short)0, (int)w_end, 0x00020000);
-        v4i held[ALIGNED ? 1 : kPieces];
-        const auto fetch = [&](int s, int8_t *to) {
+        const auto through = [&](v4i (&held)[kPieces], int s) {
 #pragma unroll
             for (int p = 0; p < kPieces; ++p) {
-                if constexpr (ALIGNED) {
-                    // a piece beyond k: an offset beyond the buffer, which reads as 0
-                    const int at = 128 * s + 16 * piece < a.k ? offset[p] : (int)0x80000000;
-                    const auto lds_at = (__attribute__((address_space(3))) void *)(to + p * 16 * kThreads + 1024 * wave);
-                    if (p < kXPieces) __builtin_amdgcn_raw_ptr_buffer_load_lds(xr, lds_at, 16, at, 128 * s, 0, 0);
-                    else __builtin_amdgcn_raw_ptr_buffer_load_lds(wr, lds_at, 16, at, 128 * s, 0, 0);
-                } else {
-                    held[p] = load_16(row[p], 128 * s + 16 * piece, a.k);
-                }
+                const int8_t *from = (p < kXPieces ? a.x : a.w) + row[p];
+                if (s < whole) __builtin_memcpy(&held[p], from + BK * s + 16 * piece, 16);
+                else held[p] = load_16(from, BK * s + 16 * piece, a.k);
             }
         };
-        const auto settle = [&](int8_t *to) {
-            if constexpr (!ALIGNED) {
+        const auto settle = [&](const v4i (&held)[kPieces], int8_t *to) {
 #pragma unroll
-                for (int p = 0; p < kPieces; ++p) *reinterpret_cast<v4i *>(to + (p * kThreads + t) * 16) = held[p];
-            }
+            for (int p = 0; p < kPieces; ++p) *reinterpret_cast<v4i *>(to + (p * kThreads + t) * 16) = held[p];
         };
 
-        v16i acc[RT][RC] = {};
-        const int at_x = (wave / WC) * 32 * RT + (lane & 31), at_w = TT + (wave % WC) * 32 * RC + (lane & 31);
-        if (steps > 0) {
-            fetch(0, lds[0]);
-            settle(lds[0]);
-        }
-        landed_and_meet<0>();
-        for (int s = 0; s < steps; ++s) {
-            const int8_t *from = lds[s & 1];
-            if (s + 1 < steps) fetch(s + 1, lds[(s + 1) & 1]);
+        const auto lay_aside = [&] {
+            if (t < TT) x_scales[t] = my_x_scale;
+            if (t < TC) w_scales[t] = my_w_scale, biases[t] = my_bias;
+        };
+        v4i acc[RT][RC] = {};
+        // operands of 64 bytes of k: the channels' in turn, a token row's in the place of the one before
+        v4i fx[RT], fw[2][RC];
+        const int row_x = (wave / WC) * 16 * RT + (lane & 15), row_w = TT + (wave % WC) * 16 * RC + (lane & 15);
+        const auto operand = [&](const int8_t *from, int at_row, int kk) {
+            return *reinterpret_cast<const v4i *>(from + at_row * BK + 16 * ((4 * kk + (lane >> 4)) ^ turned(lane & 15)));
+        };
+        const auto first_operands = [&] {
 #pragma unroll
-            for (int kk = 0; kk < 4; ++kk) {
-                const int where = 16 * ((2 * kk + (lane >> 5)) ^ (lane & 7));
-                v4i fx[RT], fw[RC];
+            for (int c = 0; c < RC; ++c) fw[0][c] = operand(place[0], row_w + 16 * c, 0);
 #pragma unroll
-                for (int r = 0; r < RT; ++r) fx[r] = *reinterpret_cast<const v4i *>(from + (at_x + 32 * r) * 128 + where);
+            for (int r = 0; r < RT; ++r) fx[r] = operand(place[0], row_x + 16 * r, 0);
+        };
+        // the step in place I, the next one's operands coming in; behind the last step they are whatever lies there, and not used
+        const auto multiply = [&](auto at) {
+            constexpr int I = decltype(at)::value;
 #pragma unroll
-                for (int c = 0; c < RC; ++c) fw[c] = *reinterpret_cast<const v4i *>(from + (at_w + 32 * c) * 128 + where);
+            for (int kk = 0; kk < kInner; ++kk) {
+                const int turn = kInner == 1 ? I & 1 : kk & 1, next = kk + 1 < kInner ? kk + 1 : 0;
+                const int8_t *from = place[kk + 1 < kInner ? I : (I + 1) % 4];
 #pragma unroll
-                for (int r = 0; r < RT; ++r)
+                for (int c = 0; c < RC; ++c) fw[turn ^ 1][c] = operand(from, row_w + 16 * c, next);
 #pragma unroll
-                    for (int c = 0; c < RC; ++c) acc[r][c] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fw[c], fx[r], acc[r][c], 0, 0, 0);
-            }
-            if (s + 1 < steps) settle(lds[(s + 1) & 1]);
-            landed_and_meet<0>();
-        }
-        // The wave's sums go through LDS of its own, 32 tokens at a time, so that its stores are whole stretches of a token's channels.
-        int *own = reinterpret_cast<int *>(&lds[0][0]) + wave * 32 * kRow;
-        const int64_t wave_i = i0 + (wave / WC) * 32 * RT, wave_j = j0 + (wave % WC) * 32 * RC;
+                for (int r = 0; r < RT; ++r) {
 #pragma unroll
-        for (int r = 0; r < RT; ++r) {
-#pragma unroll
-            for (int c = 0; c < RC; ++c)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const v4i four = {acc[r][c][4 * e], acc[r][c][4 * e + 1], acc[r][c][4 * e + 2], acc[r][c][4 * e + 3]};
-                    *reinterpret_cast<v4i *>(own + (lane & 31) * kRow + 32 * c + 8 * e + 4 * (lane >> 5)) = four;
+                    for (int c = 0; c < RC; ++c) acc[r][c] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[turn][c], fx[r], acc[r][c], 0, 0, 0);
+                    fx[r] = operand(from, row_x + 16 * r, next);
                 }
+            }
+        };
+        // four steps, each with its place as a constant
+        const auto by_four = [](auto &&one) {
+            one(std::integral_constant<int, 0>{});
+            one(std::integral_constant<int, 1>{});
+            one(std::integral_constant<int, 2>{});
+            one(std::integral_constant<int, 3>{});
+        };
+        int s = 0;
+        if constexpr (DIRECT) {
+            // bytes of the tile's rows, from its first row's beginning to its last row's end
+            const int x_bytes = (int)(((a.m - i0 < TT ? a.m - i0 : TT) - 1) * a.ldx + a.k), w_bytes = (int)(((a.n - j0 < TC ? a.n - j0 : TC) - 1) * a.ldw + a.k);
+            const auto xr = buffer_of(a.x + i0 * a.ldx, x_bytes), wr = buffer_of(a.w + j0 * a.ldw, w_bytes);
+            v4i held[kPieces];
+            if (whole < steps) through(held, whole);
+            const auto fetch = [&](int s, int8_t *to) {
+#pragma unroll
+                for (int p = 0; p < kPieces; ++p) {
+                    int8_t *at = to + p * 16 * kThreads + 1024 * wave;
+                    if (p < kXPieces) load_to_lds(xr, offset[p], BK * s, at);
+                    else load_to_lds(wr, offset[p], BK * s, at);
+                }
+            };
+            const auto prepare = [&](int s, int8_t *to) {
+                if (s < whole) fetch(s, to);
+                else if (s < steps) settle(held, to);
+            };
+            prepare(0, place[0]);
+            prepare(1, place[1]);
+            prepare(2, place[2]);
+            lay_aside();
+            if (whole >= 3) landed_and_meet<2 * kPieces>();
+            else settled_and_meet();
+            first_operands();
+            // At each step: the next one has come, and everyone is done with the one before, whose place the following loads take.  Its operands
+            // were read while the step before it was multiplied, and waited for since.
+            for (; s + 6 < whole; s += 4)
+                by_four([&](auto at) {
+                    constexpr int I = decltype(at)::value;
+                    landed_and_meet<kPieces>();
+                    fetch(s + I + 3, place[(I + 3) % 4]);
+                    multiply(at);
+                });
+            for (; s < steps; s += 4)
+                by_four([&](auto at) {
+                    constexpr int I = decltype(at)::value;
+                    if (s + I < steps) {
+                        settled_and_meet();
+                        prepare(s + I + 3, place[(I + 3) % 4]);
+                        multiply(at);
+                    }
+                });
+        } else {
+            v4i even[kPieces], odd[kPieces];        // the next step of either kind
+            if (steps > 0) through(even, 0);
+            if (steps > 1) through(odd, 1);
+            if (steps > 0) settle(even, place[0]);
+            if (steps > 2) through(even, 2);
+            if (steps > 1) settle(odd, place[1]);
+            if (steps > 3) through(odd, 3);
+            lay_aside();
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            first_operands();
+            for (; s < steps; s += 4)
+                by_four([&](auto at) {
+                    constexpr int I = decltype(at)::value;
+                    v4i(&held)[kPieces] = I & 1 ? odd : even;
+                    if (s + I < steps) {
+                        // the next step is there, and everyone is done with the one before the last, whose place the one after the next takes
+                        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+                        if (s + I + 2 < steps) settle(held, place[(I + 2) % 4]);
+                        if (s + I + 4 < steps) through(held, s + I + 4);
+                        multiply(at);
+                    }
+                });
+        }
+        settled_and_meet();
+        // The wave's sums go through LDS of its own, 32 tokens at a time, so that its stores are whole
+        // stretches of a token's channels.  A lane has the same four channels of every token.
+        constexpr int kFours = 4 * RC, kTurns = 32 * kFours / 64;
+        static_assert(RT % 2 == 0 && 64 % kFours == 0, "32 tokens at a time, a lane the same channels");
+        int8_t *const my_place = wave / kPerPlace == 0 ? place_0 : wave / kPerPlace == 1 ? place_1 : wave / kPerPlace == 2 ? place_2 : place_3;
+        int *own = reinterpret_cast<int *>(my_place) + wave % kPerPlace * 32 * kRow;
+        const int wave_t = (wave / WC) * 16 * RT, wave_c = (wave % WC) * 16 * RC + 4 * (lane % kFours);
+        const int64_t j = j0 + wave_c;
+        Channels channels;
+        channels.left = a.n - j < 4 ? (int)(a.n - j) : 4;
+        __builtin_memcpy(channels.scale, w_scales + wave_c, 16);
+        __builtin_memcpy(channels.bias, biases + wave_c, 16);
+#pragma unroll
+        for (int r = 0; r < RT; r += 2) {
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int c = 0; c < RC; ++c)
+                    *reinterpret_cast<v4i *>(own + (16 * half + (lane & 15)) * kRow + 16 * c + 4 * (lane >> 4)) = acc[r + half][c];
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
-#pragma unroll 1
-            for (int at = lane; at < 32 * 8 * RC; at += 64) {
-                const int64_t i = wave_i + 32 * r + at / (8 * RC), j = wave_j + 4 * (at % (8 * RC));
-                if (i < a.m && j < a.n) finish_4(a, i, j, *reinterpret_cast<const v4i *>(own + at / (8 * RC) * kRow + 4 * (at % (8 * RC))));
+            v4i sums[kTurns];
+            float x_scale[kTurns];
+#pragma unroll
+            for (int u = 0; u < kTurns; ++u) {
+                const int token = lane / kFours + 64 / kFours * u;
+                sums[u] = *reinterpret_cast<const v4i *>(own + token * kRow + 4 * (lane % kFours));
+                x_scale[u] = x_scales[wave_t + 16 * r + token];
+            }
+#pragma unroll
+            for (int u = 0; u < kTurns; ++u) {
+                const int64_t i = i0 + wave_t + 16 * r + lane / kFours + 64 / kFours * u;
+                if (i < a.m && channels.left > 0) finish_4(a, i, j, sums[u], x_scale[u], channels);
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
         }
-        __syncthreads();
+        if (id + gridDim.x < tiles) settled_and_meet();       // before the next tile's loads
     }
 }
 
@@ -218,6 +335,18 @@ __global__ void __launch_bounds__(512) dense_few_kernel(DenseClearArgs a) {
         for (int r = 0; r < RT; ++r) {
             const int64_t i = 16 * r + (lane & 15);
             x[r] = i < a.m ? a.x + i * a.ldx + part : nullptr;
+        }
+        // what the outputs take, asked for before the weights
+        const int64_t my_i = 16 * wave + (lane & 15), my_j = group * 16 + 4 * (lane >> 4);
+        Channels channels = {};
+        float x_scale = 1.0f;
+        if (wave < RT) {
+            channels = {{1.0f, 1.0f, 1.0f, 1.0f}, {0, 0, 0, 0}, a.n - my_j < 4 ? (int)(a.n - my_j) : 4};
+            if (channels.left > 0) {
+                if (a.w_scale) load_4(channels.scale, a.w_scale + my_j, channels.left);
+                if (a.bias) load_4(channels.bias, static_cast<const int *>(a.bias) + my_j, channels.left);
+            }
+            if (a.x_scale && my_i < a.m) x_scale = a.x_scale[my_i];
         }
         v4i acc[RT] = {};
         // wave w: blocks w * each ... of k, and the last wave what is left of less than a block
@@ -251,12 +380,10 @@ __global__ void __launch_bounds__(512) dense_few_kernel(DenseClearArgs a) {
 #pragma unroll
         for (int r = 0; r < RT; ++r) sums[wave][r][lane] = acc[r];
         __syncthreads();
-        if (t < 64 * RT) {
-            const int r = t >> 6;
-            v4i s = sums[0][r][lane];
-            for (int v = 1; v < kWaves; ++v) s += sums[v][r][lane];
-            const int64_t i = 16 * r + (lane & 15), first = group * 16 + 4 * (lane >> 4);
-            if (i < a.m && first < a.n) finish_4(a, i, first, s);
+        if (wave < RT && my_i < a.m && channels.left > 0) {
+            v4i s = sums[0][wave][lane];
+            for (int v = 1; v < kWaves; ++v) s += sums[v][wave][lane];
+            finish_4(a, my_i, my_j, s, x_scale, channels);
         }
         __syncthreads();
     }
@@ -266,17 +393,17 @@ __global__ void __launch_bounds__(512) dense_few_kernel(DenseClearArgs a) {
 constexpr int64_t kMostGroups = 1 << 20;
 static dim3 groups_of(int64_t tiles) { return dim3((unsigned)(tiles < kMostGroups ? tiles : kMostGroups)); }
 
-template <int WT, int WC, int RT, int RC>
-static void tile_launch(const DenseClearArgs &a, bool aligned, hipStream_t stream) {
-    const int64_t tiles = ((a.n + 32 * WC * RC - 1) / (32 * WC * RC)) * ((a.m + 32 * WT * RT - 1) / (32 * WT * RT));
-    if (aligned) dense_tile_kernel<WT, WC, RT, RC, true><<<groups_of(tiles), 64 * WT * WC, 0, stream>>>(a);
-    else dense_tile_kernel<WT, WC, RT, RC, false><<<groups_of(tiles), 64 * WT * WC, 0, stream>>>(a);
+template <int WT, int WC, int RT, int RC, int BK>
+static void tile_launch(const DenseClearArgs &a, bool direct, hipStream_t stream) {
+    constexpr int TT = 16 * WT * RT, TC = 16 * WC * RC;
+    const int64_t tiles = ((a.n + TC - 1) / TC) * ((a.m + TT - 1) / TT);
+    if (direct) dense_tile_kernel<WT, WC, RT, RC, BK, true><<<groups_of(tiles), 64 * WT * WC, 0, stream>>>(a);
+    else dense_tile_kernel<WT, WC, RT, RC, BK, false><<<groups_of(tiles), 64 * WT * WC, 0, stream>>>(a);
 }
 
 static void dense_launch(const DenseClearArgs &a, hipStream_t stream) {
-    // FORM-BEGIN
-    const auto sixteen = [](const void *p, int64_t ld) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 16 == 0 && ld <= 1 << 22; };
-    const bool aligned = a.k % 16 == 0 && sixteen(a.x, a.ldx) && sixteen(a.w, a.ldw);
+    const auto fours = [](const void *p, int64_t ld) { return reinterpret_cast<uintptr_t>(p) % 4 == 0 && ld % 4 == 0 && ld <= 1 << 22; };
+    const bool direct = fours(a.x, a.ldx) && fours(a.w, a.ldw);
     const auto tiles = [&](int64_t side) { return ((a.m + side - 1) / side) * ((a.n + side - 1) / side); };
     int form = a.m <= 16 ? 1 : a.m <= 32 ? 2 : a.m <= 64 ? 3 : tiles(256) >= 192 ? 6 : tiles(128) >= 192 ? 5 : 4;
     // FORM-END
@@ -284,9 +411,17 @@ static void dense_launch(const DenseClearArgs &a, hipStream_t stream) {
         case 1: dense_few_kernel<1><<<groups_of((a.n + 15) / 16), 512, 0, stream>>>(a); break;
         case 2: dense_few_kernel<2><<<groups_of((a.n + 15) / 16), 512, 0, stream>>>(a); break;
         case 3: dense_few_kernel<4><<<groups_of((a.n + 15) / 16), 512, 0, stream>>>(a); break;
-        case 4: tile_launch<2, 2, 1, 1>(a, aligned, stream); break;
-        case 5: tile_launch<2, 2, 2, 2>(a, aligned, stream); break;
-        default: tile_launch<2, 4, 4, 2>(a, aligned, stream); break;
+        case 4: tile_launch<2, 2, 2, 2, 128>(a, direct, stream); break;
+        case 5: tile_launch<2, 2, 4, 4, 64>(a, direct, stream); break;
+#ifdef PROBE
+        case 10: tile_launch<2, 4, 2, 2, 128>(a, direct, stream); break;
+        case 12: tile_launch<2, 2, 8, 8, 64>(a, direct, stream); break;
+        case 13: tile_launch<2, 4, 4, 4, 64>(a, direct, stream); break;
+        case 14: tile_launch<2, 4, 4, 2, 64>(a, direct, stream); break;
+        case 15: tile_launch<4, 2, 4, 4, 64>(a, direct, stream); break;
+        case 16: tile_launch<2, 4, 4, 2, 128>(a, direct, stream); break;
+#endif
+        default: tile_launch<2, 4, 8, 4, 64>(a, direct, stream); break;
     }
 }
 

@@ -26,6 +26,7 @@ def call(name, base, **change):
     (dict(kind=-1), PARAM, "kind"), (dict(kind=6), PARAM, "kind"),
     (dict(m=-1), SIZE, "rows"), (dict(k=-1), SIZE, "rows"), (dict(n=-1), SIZE, "channels"),
     (dict(m=2**31), SIZE, "rows"), (dict(n=2**31), SIZE, "channels"), (dict(n=2**63 - 1), SIZE, "channels"),
+    (dict(m=2**31 - 1, n=2**31 - 1, ldo=2**31), SIZE, "too many"),
     (dict(k=131072, ldx=131072, ldw=131072), SIZE, "at most 131071"), (dict(k=2**32 + 64, ldx=2**33, ldw=2**33), SIZE, "at most"),
     (dict(ldx=63), SIZE, "stride"), (dict(ldw=63), SIZE, "stride"), (dict(ldo=31), SIZE, "stride"), (dict(ldx=-64), SIZE, "stride"),
     (dict(ldx=2**41), SIZE, "stride"),

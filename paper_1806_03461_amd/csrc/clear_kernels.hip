@@ -199,6 +199,8 @@ __global__ void __launch_bounds__(64 * WT * WC, RT * RC == 64 ? 1 : 2) dense_til
 #pragma unroll
                     for (int c = 0; c < RC; ++c) acc[r][c] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[turn][c], fx[r], acc[r][c], 0, 0, 0);
                     fx[r] = operand(from, row_x + 16 * r, next);
+                    // left to itself the compiler reads just before use, and lets products of the next step pass the border
+                    __builtin_amdgcn_sched_barrier(0);
                 }
             }
         };

@@ -10,11 +10,17 @@ typedef int v4i __attribute__((ext_vector_type(4)));
 
 // ---- the product ---------------------------------------------------------------------------------------------------
 
-// 16 bytes of a row from byte `at` on, of which only those before `k` count: the rest is 0 and not read.
+// 16 bytes of a row from byte `at` on, of which only those before `k` count: the rest is 0 and not read.  At the row's end the last
+// 16 bytes are read and shifted down, one load in any case.
 __device__ __forceinline__ v4i load_16(const int8_t *row, int at, int k) {
     v4i v = {0, 0, 0, 0};
-    if (at + 16 <= k) {
-        __builtin_memcpy(&v, row + at, 16);
+    if (k >= 16) {
+        const int from = std::min(at, k - 16), bits = 8 * std::min(at - from, 16);
+        uint64_t half[2];
+        __builtin_memcpy(half, row + from, 16);
+        if (bits >= 64) half[0] = bits < 128 ? half[1] >> (bits - 64) : 0, half[1] = 0;
+        else if (bits > 0) half[0] = half[0] >> bits | half[1] << (64 - bits), half[1] >>= bits;
+        __builtin_memcpy(&v, half, 16);
     } else {
         for (int j = 0; j < 16; ++j)
             if (at + j < k) v[j >> 2] |= (int)(uint8_t)row[at + j] << (8 * (j & 3));
@@ -145,22 +151,20 @@ __global__ void __launch_bounds__(64 * WT * WC, RT * RC == 64 ? 1 : 2) dense_til
         const int my_bias = w_mine && a.bias ? static_cast<const int *>(a.bias)[j0 + t] : 0;
         // piece p of a thread: row p * kRows + t / kPerRow of the tile's tokens, then of its channels
         const int my_row = t / kPerRow, piece = t % kPerRow ^ turned(my_row);
-        int64_t row[kPieces];
-        int offset[kPieces];
+        std::conditional_t<DIRECT, int, int64_t> offset[kPieces];       // from the tile's first row
 #pragma unroll
         for (int p = 0; p < kPieces; ++p) {
             const bool is_x = p < kXPieces;
-            const int64_t r = (is_x ? i0 : j0) + (p - (is_x ? 0 : kXPieces)) * kRows + my_row, rows = is_x ? a.m : a.n;
-            const int64_t kept = r < rows ? r : rows - 1;       // beyond the last row: that row again, never stored
-            row[p] = kept * (is_x ? a.ldx : a.ldw);
-            if (DIRECT) offset[p] = (int)(row[p] - (is_x ? i0 * a.ldx : j0 * a.ldw)) + 16 * piece;
+            const int64_t r = (p - (is_x ? 0 : kXPieces)) * kRows + my_row, rows = is_x ? a.m - i0 : a.n - j0;
+            offset[p] = (r < rows ? r : rows - 1) * (is_x ? a.ldx : a.ldw) + 16 * piece;    // beyond the last row: that row again, never stored
         }
-        const auto through = [&](v4i (&held)[kPieces], int s) {
+        const int8_t *const x_rows = a.x + i0 * a.ldx, *const w_rows = a.w + j0 * a.ldw;
+        const auto through = [&](v4i (&held)[kPieces], int s, auto... is_whole) {
 #pragma unroll
             for (int p = 0; p < kPieces; ++p) {
-                const int8_t *from = (p < kXPieces ? a.x : a.w) + row[p];
-                if (s < whole) __builtin_memcpy(&held[p], from + BK * s + 16 * piece, 16);
-                else held[p] = load_16(from, BK * s + 16 * piece, a.k);
+                const int8_t *from = (p < kXPieces ? x_rows : w_rows) + offset[p];
+                if ((is_whole || ... || (s < whole))) __builtin_memcpy(&held[p], from + BK * s, 16);
+                else held[p] = load_16(from - 16 * piece, BK * s + 16 * piece, a.k);
             }
         };
         const auto settle = [&](const v4i (&held)[kPieces], int8_t *to) {
@@ -215,9 +219,9 @@ __global__ void __launch_bounds__(64 * WT * WC, RT * RC == 64 ? 1 : 2) dense_til
         if constexpr (DIRECT) {
             // bytes of the tile's rows, from its first row's beginning to its last row's end
             const int x_bytes = (int)(((a.m - i0 < TT ? a.m - i0 : TT) - 1) * a.ldx + a.k), w_bytes = (int)(((a.n - j0 < TC ? a.n - j0 : TC) - 1) * a.ldw + a.k);
-            const auto xr = buffer_of(a.x + i0 * a.ldx, x_bytes), wr = buffer_of(a.w + j0 * a.ldw, w_bytes);
-            v4i held[kPieces];
-            if (whole < steps) through(held, whole);
+            const auto xr = buffer_of(x_rows, x_bytes), wr = buffer_of(w_rows, w_bytes);
+            constexpr bool kEarly = RT * RC < 16;                  // registers for the last, partial step from the start on
+            v4i held[kEarly ? kPieces : 1];
             const auto fetch = [&](int s, int8_t *to) {
 #pragma unroll
                 for (int p = 0; p < kPieces; ++p) {
@@ -227,9 +231,20 @@ __global__ void __launch_bounds__(64 * WT * WC, RT * RC == 64 ? 1 : 2) dense_til
                 }
             };
             const auto prepare = [&](int s, int8_t *to) {
-                if (s < whole) fetch(s, to);
-                else if (s < steps) settle(held, to);
+                if (s < whole) {
+                    fetch(s, to);
+                } else if (s < steps) {
+                    if constexpr (kEarly) {
+                        settle(held, to);
+                    } else {
+                        v4i now[kPieces];
+                        through(now, s);
+                        settle(now, to);
+                    }
+                }
             };
+            if constexpr (kEarly)
+                if (whole < steps) through(held, whole);
             prepare(0, place[0]);
             prepare(1, place[1]);
             prepare(2, place[2]);
@@ -256,28 +271,34 @@ __global__ void __launch_bounds__(64 * WT * WC, RT * RC == 64 ? 1 : 2) dense_til
                     }
                 });
         } else {
-            v4i even[kPieces], odd[kPieces];        // the next step of either kind
-            if (steps > 0) through(even, 0);
-            if (steps > 1) through(odd, 1);
-            if (steps > 0) settle(even, place[0]);
-            if (steps > 2) through(even, 2);
-            if (steps > 1) settle(odd, place[1]);
-            if (steps > 3) through(odd, 3);
+            constexpr int kSets = RT * RC >= 16 ? 2 : 4;            // steps under way to registers, as many as there is room for
+            v4i held[kSets][kPieces];
+#pragma unroll
+            for (int h = 0; h < kSets; ++h)
+                if (h < steps) through(held[h], h);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (h < steps) settle(held[h], place[h]);
+                if (h + kSets < steps) through(held[h], h + kSets);
+            }
             lay_aside();
             asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
             first_operands();
-            for (; s < steps; s += 4)
+            // without conditions as long as there are whole steps, or the compiler would not know how many loads it may leave under way
+            const auto four_steps = [&](auto all) {
                 by_four([&](auto at) {
-                    constexpr int I = decltype(at)::value;
-                    v4i(&held)[kPieces] = I & 1 ? odd : even;
-                    if (s + I < steps) {
+                    constexpr int I = decltype(at)::value, kSet = (I + 2) % kSets;
+                    if (all || s + I < steps) {
                         // the next step is there, and everyone is done with the one before the last, whose place the one after the next takes
                         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-                        if (s + I + 2 < steps) settle(held, place[(I + 2) % 4]);
-                        if (s + I + 4 < steps) through(held, s + I + 4);
+                        if (all || s + I + 2 < steps) settle(held[kSet], place[(I + 2) % 4]);
+                        if (all || s + I + 2 + kSets < steps) through(held[kSet], s + I + 2 + kSets, all);
                         multiply(at);
                     }
                 });
+            };
+            for (; s + 5 + kSets < whole; s += 4) four_steps(std::true_type{});
+            for (; s < steps; s += 4) four_steps(std::false_type{});
         }
         settled_and_meet();
         // The wave's sums go through LDS of its own, 32 tokens at a time, so that its stores are whole
@@ -321,28 +342,34 @@ __global__ void __launch_bounds__(64 * WT * WC, RT * RC == 64 ? 1 : 2) dense_til
     }
 }
 
-// Few tokens (up to 16 RT): the weights are read once and that is what it costs.  A workgroup takes 16 channels, its eight waves
-// 64-byte blocks of k in turn; the weights go from memory to the products' registers without LDS, the waves' sums meet there.
-template <int RT>
-__global__ void __launch_bounds__(512) dense_few_kernel(DenseClearArgs a) {
-    constexpr int kWaves = 8, kAhead = RT == 1 ? 8 : 4;
-    __shared__ v4i sums[kWaves][RT][64];
-    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
-    const int64_t groups = (a.n + 15) / 16;
+// Few tokens (up to 16 RT): the weights are read once and that is what it costs.  A workgroup takes 16 RC channels, its waves
+// consecutive parts of k, 64 bytes at a time; the weights go from memory to the products' registers without LDS, the waves' sums meet there.
+template <int RT, int RC, int AHEAD, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES) dense_few_kernel(DenseClearArgs a) {
+    static_assert(RT * RC <= WAVES, "a wave a tile of the sums");
+    __shared__ v4i sums[WAVES][RT * RC][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const unsigned groups = (unsigned)((a.n + 16 * RC - 1) / (16 * RC));
     const int blocks = a.k / 64, part = 16 * (lane >> 4);
-    for (int64_t group = blockIdx.x; group < groups; group += gridDim.x) {
-        const int64_t j = group * 16 + (lane & 15), kept = j < a.n ? j : a.n - 1;
-        const int8_t *w = a.w + kept * a.ldw + part;
-        const int8_t *x[RT];
+    for (unsigned group = blockIdx.x; group < groups; group += gridDim.x) {
+        const int64_t first = (int64_t)group * 16 * RC;
+        const int8_t *w[RC], *x[RT];
+#pragma unroll
+        for (int c = 0; c < RC; ++c) {
+            const int64_t j = first + 16 * c + (lane & 15);
+            w[c] = a.w + (j < a.n ? j : a.n - 1) * a.ldw + part;
+        }
+#pragma unroll
         for (int r = 0; r < RT; ++r) {
+            // beyond the last token: that one again, never stored
             const int64_t i = 16 * r + (lane & 15);
-            x[r] = i < a.m ? a.x + i * a.ldx + part : nullptr;
+            x[r] = a.x + (i < a.m ? i : a.m - 1) * a.ldx + part;
         }
         // what the outputs take, asked for before the weights
-        const int64_t my_i = 16 * wave + (lane & 15), my_j = group * 16 + 4 * (lane >> 4);
+        const int64_t my_i = 16 * (wave / RC) + (lane & 15), my_j = first + 16 * (wave % RC) + 4 * (lane >> 4);
         Channels channels = {};
         float x_scale = 1.0f;
-        if (wave < RT) {
+        if (wave < RT * RC) {
             channels = {{1.0f, 1.0f, 1.0f, 1.0f}, {0, 0, 0, 0}, a.n - my_j < 4 ? (int)(a.n - my_j) : 4};
             if (channels.left > 0) {
                 if (a.w_scale) load_4(channels.scale, a.w_scale + my_j, channels.left);
@@ -350,41 +377,50 @@ __global__ void __launch_bounds__(512) dense_few_kernel(DenseClearArgs a) {
             }
             if (a.x_scale && my_i < a.m) x_scale = a.x_scale[my_i];
         }
-        v4i acc[RT] = {};
-        // wave w: blocks w * each ... of k, and the last wave what is left of less than a block
-        const int each = (blocks + kWaves - 1) / kWaves, last = (wave + 1) * each < blocks ? (wave + 1) * each : blocks;
-        for (int b = wave * each; b < last; b += kAhead) {
-            v4i fw[kAhead], fx[kAhead][RT];
+        v4i acc[RT][RC] = {};
+        const auto some = [&](auto count, int b) {
+            constexpr int kCount = decltype(count)::value;
+            v4i fw[kCount][RC], fx[kCount][RT];
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) {
-                const int at = 64 * (b + u < last ? b + u : last - 1);
-                __builtin_memcpy(&fw[u], w + at, 16);
+            for (int u = 0; u < kCount; ++u) {
 #pragma unroll
-                for (int r = 0; r < RT; ++r) {
-                    fx[u][r] = v4i{0, 0, 0, 0};
-                    if (x[r] && b + u < last) __builtin_memcpy(&fx[u][r], x[r] + at, 16);
-                }
+                for (int c = 0; c < RC; ++c) __builtin_memcpy(&fw[u][c], w[c] + 64 * (b + u), 16);
+#pragma unroll
+                for (int r = 0; r < RT; ++r) __builtin_memcpy(&fx[u][r], x[r] + 64 * (b + u), 16);
             }
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u)
+            for (int u = 0; u < kCount; ++u)
 #pragma unroll
-                for (int r = 0; r < RT; ++r) acc[r] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[u], fx[u][r], acc[r], 0, 0, 0);
-        }
-        if (wave == kWaves - 1 && blocks * 64 < a.k) {
+                for (int r = 0; r < RT; ++r)
+#pragma unroll
+                    for (int c = 0; c < RC; ++c) acc[r][c] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[u][c], fx[u][r], acc[r][c], 0, 0, 0);
+        };
+        // wave w: blocks w * each ... of k, and the last wave what is left of less than a block
+        const int each = (blocks + WAVES - 1) / WAVES, last = std::min((wave + 1) * each, blocks);
+        int b = wave * each;
+        for (; b + AHEAD <= last; b += AHEAD) some(std::integral_constant<int, AHEAD>{}, b);
+        for (; b < last; ++b) some(std::integral_constant<int, 1>{}, b);
+        if (wave == WAVES - 1 && blocks * 64 < a.k) {
             const int at = blocks * 64 + part;
-            const v4i fw = load_16(w - part, at, a.k);
+            v4i fw[RC];
+#pragma unroll
+            for (int c = 0; c < RC; ++c) fw[c] = load_16(w[c] - part, at, a.k);
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
-                const v4i fx = x[r] ? load_16(x[r] - part, at, a.k) : v4i{0, 0, 0, 0};
-                acc[r] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw, fx, acc[r], 0, 0, 0);
+                const v4i fx = load_16(x[r] - part, at, a.k);
+#pragma unroll
+                for (int c = 0; c < RC; ++c) acc[r][c] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[c], fx, acc[r][c], 0, 0, 0);
             }
         }
 #pragma unroll
-        for (int r = 0; r < RT; ++r) sums[wave][r][lane] = acc[r];
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int c = 0; c < RC; ++c) sums[wave][r * RC + c][lane] = acc[r][c];
         __syncthreads();
-        if (wave < RT && my_i < a.m && channels.left > 0) {
+        if (wave < RT * RC && my_i < a.m && channels.left > 0) {
             v4i s = sums[0][wave][lane];
-            for (int v = 1; v < kWaves; ++v) s += sums[v][wave][lane];
+#pragma unroll
+            for (int v = 1; v < WAVES; ++v) s += sums[v][wave][lane];
             finish_4(a, my_i, my_j, s, x_scale, channels);
         }
         __syncthreads();
@@ -395,34 +431,63 @@ __global__ void __launch_bounds__(512) dense_few_kernel(DenseClearArgs a) {
 constexpr int64_t kMostGroups = 1 << 20;
 static dim3 groups_of(int64_t tiles) { return dim3((unsigned)(tiles < kMostGroups ? tiles : kMostGroups)); }
 
+template <int RT, int RC, int AHEAD, int WAVES>
+static void few_launch(const DenseClearArgs &a, hipStream_t stream) {
+    dense_few_kernel<RT, RC, AHEAD, WAVES><<<groups_of((a.n + 16 * RC - 1) / (16 * RC)), 64 * WAVES, 0, stream>>>(a);
+}
+
 template <int WT, int WC, int RT, int RC, int BK>
 static void tile_launch(const DenseClearArgs &a, bool direct, hipStream_t stream) {
     constexpr int TT = 16 * WT * RT, TC = 16 * WC * RC;
     const int64_t tiles = ((a.n + TC - 1) / TC) * ((a.m + TT - 1) / TT);
-    if (direct) dense_tile_kernel<WT, WC, RT, RC, BK, true><<<groups_of(tiles), 64 * WT * WC, 0, stream>>>(a);
-    else dense_tile_kernel<WT, WC, RT, RC, BK, false><<<groups_of(tiles), 64 * WT * WC, 0, stream>>>(a);
+    if (direct) {
+        dense_tile_kernel<WT, WC, RT, RC, BK, true><<<groups_of(tiles), 64 * WT * WC, 0, stream>>>(a);
+    } else if constexpr (RT * RC < 32) {
+        dense_tile_kernel<WT, WC, RT, RC, BK, false><<<groups_of(tiles), 64 * WT * WC, 0, stream>>>(a);
+    }
+}
+
+// The tile kernel's forms, and what a launch of each takes: with up to 256, 512, 768 tiles -- one, two, three on a CU, as many as its LDS
+// holds -- a start and end of `fixed` and `step` for 128 bytes of k, in us, measured as kernels of 4096-byte and 1024-byte rows in a
+// captured sequence.  More tiles than a device holds at once go round, a round after the first at the cost of its steps and two thirds of its start.
+struct TileForm {
+    int tokens, channels, at_once;
+    struct { float fixed, step; } cost[3];
+};
+constexpr TileForm kTileForms[] = {
+    {32, 64, 3, {{3.1f, 0.249f}, {4.1f, 0.290f}, {4.9f, 0.418f}}},
+    {64, 64, 2, {{4.0f, 0.271f}, {5.1f, 0.394f}}},
+    {64, 128, 1, {{5.4f, 0.320f}}},
+    {128, 128, 1, {{7.1f, 0.473f}}},
+    {256, 128, 1, {{9.9f, 1.000f}}},
+    {256, 256, 1, {{16.4f, 1.610f}}}};
+
+static float tile_cost(const TileForm &f, const DenseClearArgs &a) {
+    const float steps = (float)a.k / 128.0f;
+    const int64_t tiles = ((a.m + f.tokens - 1) / f.tokens) * ((a.n + f.channels - 1) / f.channels), on_cu = (tiles + 255) / 256;
+    const int64_t rounds = (on_cu - 1) / f.at_once, rest = on_cu - rounds * f.at_once;
+    const auto &full = f.cost[f.at_once - 1], &last = f.cost[rest - 1];
+    return last.fixed + last.step * steps + (float)rounds * (0.67f * full.fixed + full.step * steps);
 }
 
 static void dense_launch(const DenseClearArgs &a, hipStream_t stream) {
     const auto fours = [](const void *p, int64_t ld) { return reinterpret_cast<uintptr_t>(p) % 4 == 0 && ld % 4 == 0 && ld <= 1 << 22; };
     const bool direct = fours(a.x, a.ldx) && fours(a.w, a.ldw);
-    const auto tiles = [&](int64_t side) { return ((a.m + side - 1) / side) * ((a.n + side - 1) / side); };
-    int form = a.m <= 16 ? 1 : a.m <= 32 ? 2 : a.m <= 64 ? 3 : tiles(256) >= 192 ? 6 : tiles(128) >= 192 ? 5 : 4;
+    // Up to 16 tokens read each weight once; so do up to 32 if the channels are few enough that tiles would leave CUs idle
+    // (24 tokens, 4096 -> 4096 8.2 us, tiles 10.7; 4096 -> 8192 12.8 and 11.1).
+    if (a.m <= 16) return few_launch<1, 1, 2, 8>(a, stream);
+    if (a.m <= 32 && a.n <= 4096) return few_launch<2, 1, 4, 8>(a, stream);
+    // Through registers the largest has none left (2001-byte rows, 4000 x 4000: 73 us, and 82 with the one before), rows a few bytes long aside.
+    int form = 0;
+    for (int f = 1; f < (direct ? 6 : 5); ++f)
+        if (tile_cost(kTileForms[f], a) < tile_cost(kTileForms[form], a)) form = f;
     // FORM-END
     switch (form) {
-        case 1: dense_few_kernel<1><<<groups_of((a.n + 15) / 16), 512, 0, stream>>>(a); break;
-        case 2: dense_few_kernel<2><<<groups_of((a.n + 15) / 16), 512, 0, stream>>>(a); break;
-        case 3: dense_few_kernel<4><<<groups_of((a.n + 15) / 16), 512, 0, stream>>>(a); break;
-        case 4: tile_launch<2, 2, 2, 2, 128>(a, direct, stream); break;
-        case 5: tile_launch<2, 2, 4, 4, 64>(a, direct, stream); break;
-#ifdef PROBE
-        case 10: tile_launch<2, 4, 2, 2, 128>(a, direct, stream); break;
-        case 12: tile_launch<2, 2, 8, 8, 64>(a, direct, stream); break;
-        case 13: tile_launch<2, 4, 4, 4, 64>(a, direct, stream); break;
-        case 14: tile_launch<2, 4, 4, 2, 64>(a, direct, stream); break;
-        case 15: tile_launch<4, 2, 4, 4, 64>(a, direct, stream); break;
-        case 16: tile_launch<2, 4, 4, 2, 128>(a, direct, stream); break;
-#endif
+        case 0: tile_launch<1, 4, 2, 1, 128>(a, direct, stream); break;
+        case 1: tile_launch<2, 2, 2, 2, 128>(a, direct, stream); break;
+        case 2: tile_launch<2, 4, 2, 2, 128>(a, direct, stream); break;
+        case 3: tile_launch<2, 4, 4, 2, 128>(a, direct, stream); break;
+        case 4: tile_launch<4, 2, 4, 4, 64>(a, direct, stream); break;
         default: tile_launch<2, 4, 8, 4, 64>(a, direct, stream); break;
     }
 }

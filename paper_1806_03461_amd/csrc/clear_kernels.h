@@ -13,6 +13,7 @@ struct DenseClearArgs {
     int64_t m, n;
     int k;
     int kind;                       // BNN_CLEAR_F32 ... BNN_CLEAR_BITS
+    bool past;                      // set by the launcher: stores past the caches' order of what to keep
 };
 
 struct RowsClearArgs {

@@ -8,6 +8,12 @@ namespace tfhe {
 
 typedef int v4i __attribute__((ext_vector_type(4)));
 
+// The same value, but for the compiler another: what follows from it is computed anew, not kept in registers from before.
+__device__ __forceinline__ int again(int v) {
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
 // ---- the product ---------------------------------------------------------------------------------------------------
 
 // 16 bytes of a row from byte `at` on, of which only those before `k` count: the rest is 0 and not read.  At the row's end the last
@@ -40,9 +46,15 @@ __device__ __forceinline__ void load_4(T (&v)[4], const T *p, int left) {
     }
 }
 
+// past: past the caches' order of what to keep
 template <class T>
-__device__ __forceinline__ void store_4(T *p, const T (&v)[4], int left) {
-    if (left == 4) {
+__device__ __forceinline__ void store_4(T *p, const T (&v)[4], int left, bool past) {
+    typedef unsigned char Bytes __attribute__((ext_vector_type(sizeof v), aligned(sizeof(T))));
+    if (left == 4 && past) {
+        Bytes b;
+        __builtin_memcpy(&b, v, sizeof v);
+        __builtin_nontemporal_store(b, reinterpret_cast<Bytes *>(p));
+    } else if (left == 4) {
         __builtin_memcpy(p, v, sizeof v);
     } else {
 #pragma unroll
@@ -65,27 +77,27 @@ __device__ __forceinline__ void finish_4(const DenseClearArgs &a, int64_t i, int
         if (a.kind == BNN_CLEAR_I32) {
             int o[4];
             for (int e = 0; e < 4; ++e) o[e] = (int)((unsigned)acc[e] + (unsigned)c.bias[e]);
-            store_4(static_cast<int *>(a.out) + at, o, c.left);
+            store_4(static_cast<int *>(a.out) + at, o, c.left, a.past);
         } else {
             const int8_t no = a.kind == BNN_CLEAR_SIGN ? -1 : 0;
             int8_t o[4];
             for (int e = 0; e < 4; ++e) o[e] = (int64_t)acc[e] + c.bias[e] >= 0 ? (int8_t)1 : no;
-            store_4(static_cast<int8_t *>(a.out) + at, o, c.left);
+            store_4(static_cast<int8_t *>(a.out) + at, o, c.left, a.past);
         }
         return;
     }
     float y[4];
     for (int e = 0; e < 4; ++e) y[e] = (float)acc[e] * x_scale * c.scale[e] + __int_as_float(c.bias[e]);
     if (a.kind == BNN_CLEAR_F32) {
-        store_4(static_cast<float *>(a.out) + at, y, c.left);
+        store_4(static_cast<float *>(a.out) + at, y, c.left, a.past);
     } else if (a.kind == BNN_CLEAR_BF16) {
         __bf16 o[4];
         for (int e = 0; e < 4; ++e) o[e] = (__bf16)y[e];
-        store_4(static_cast<__bf16 *>(a.out) + at, o, c.left);
+        store_4(static_cast<__bf16 *>(a.out) + at, o, c.left, a.past);
     } else {
         _Float16 o[4];
         for (int e = 0; e < 4; ++e) o[e] = (_Float16)y[e];
-        store_4(static_cast<_Float16 *>(a.out) + at, o, c.left);
+        store_4(static_cast<_Float16 *>(a.out) + at, o, c.left, a.past);
     }
 }
 
@@ -134,11 +146,12 @@ __global__ void __launch_bounds__(64 * WT * WC, RT * RC == 64 ? 1 : 2) dense_til
     __shared__ __attribute__((aligned(16))) float x_scales[TT], w_scales[TC];
     __shared__ __attribute__((aligned(16))) int biases[TC];
     static_assert(TT <= kThreads && TC <= kThreads, "a thread a token or channel");
-    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const unsigned across = (unsigned)((a.n + TC - 1) / TC), down = (unsigned)((a.m + TT - 1) / TT), tiles = across * down;
     const int whole = a.k / BK, steps = (a.k + BK - 1) / BK;
     const auto turned = [](int row) { return BK == 128 ? row & 7 : (row >> 1) & 3; };
     for (unsigned id = blockIdx.x; id < tiles; id += gridDim.x) {
+        // (found anew for each tile: kept from one to the next, addresses would take registers from the sums)
+        const int t = again(threadIdx.x), lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
         // Workgroups go round the eight XCDs; each XCD gets neighbouring tiles, four token tiles by all channels at a time, so that
         // its L2 is asked for the same rows.
         const unsigned xcd = id & 7, share = tiles >> 3, over = tiles & 7, lin = xcd * share + std::min(xcd, over) + (id >> 3);
@@ -151,13 +164,16 @@ __global__ void __launch_bounds__(64 * WT * WC, RT * RC == 64 ? 1 : 2) dense_til
         const int my_bias = w_mine && a.bias ? static_cast<const int *>(a.bias)[j0 + t] : 0;
         // piece p of a thread: row p * kRows + t / kPerRow of the tile's tokens, then of its channels
         const int my_row = t / kPerRow, piece = t % kPerRow ^ turned(my_row);
-        std::conditional_t<DIRECT, int, int64_t> offset[kPieces];       // from the tile's first row
+        const int x_last = (int)std::min<int64_t>(a.m - i0, TT) - 1, w_last = (int)std::min<int64_t>(a.n - j0, TC) - 1;
+        using Offset = std::conditional_t<DIRECT, int, int64_t>;        // from the tile's first row; strides are small if DIRECT
+        const auto row_offset = [&](int p) {
+            // beyond the last row: that row again, never stored
+            return p < kXPieces ? (Offset)std::min(p * kRows + my_row, x_last) * (Offset)a.ldx
+                                : (Offset)std::min((p - kXPieces) * kRows + my_row, w_last) * (Offset)a.ldw;
+        };
+        Offset offset[kPieces];
 #pragma unroll
-        for (int p = 0; p < kPieces; ++p) {
-            const bool is_x = p < kXPieces;
-            const int64_t r = (p - (is_x ? 0 : kXPieces)) * kRows + my_row, rows = is_x ? a.m - i0 : a.n - j0;
-            offset[p] = (r < rows ? r : rows - 1) * (is_x ? a.ldx : a.ldw) + 16 * piece;    // beyond the last row: that row again, never stored
-        }
+        for (int p = 0; p < kPieces; ++p) offset[p] = row_offset(p) + 16 * piece;
         const int8_t *const x_rows = a.x + i0 * a.ldx, *const w_rows = a.w + j0 * a.ldw;
         const auto through = [&](v4i (&held)[kPieces], int s, auto... is_whole) {
 #pragma unroll
@@ -218,7 +234,7 @@ __global__ void __launch_bounds__(64 * WT * WC, RT * RC == 64 ? 1 : 2) dense_til
         int s = 0;
         if constexpr (DIRECT) {
             // bytes of the tile's rows, from its first row's beginning to its last row's end
-            const int x_bytes = (int)(((a.m - i0 < TT ? a.m - i0 : TT) - 1) * a.ldx + a.k), w_bytes = (int)(((a.n - j0 < TC ? a.n - j0 : TC) - 1) * a.ldw + a.k);
+            const int x_bytes = x_last * (int)a.ldx + a.k, w_bytes = w_last * (int)a.ldw + a.k;
             const auto xr = buffer_of(x_rows, x_bytes), wr = buffer_of(w_rows, w_bytes);
             constexpr bool kEarly = RT * RC < 16;                  // registers for the last, partial step from the start on
             v4i held[kEarly ? kPieces : 1];
@@ -237,9 +253,14 @@ __global__ void __launch_bounds__(64 * WT * WC, RT * RC == 64 ? 1 : 2) dense_til
                     if constexpr (kEarly) {
                         settle(held, to);
                     } else {
-                        v4i now[kPieces];
-                        through(now, s);
-                        settle(now, to);
+                        const int late = again(t);
+#pragma unroll 1
+                        for (int p = 0; p < kPieces; ++p) {
+                            const int r = late / kPerRow, piece = late % kPerRow ^ turned(r);
+                            const int8_t *from = p < kXPieces ? x_rows + (int64_t)std::min(p * kRows + r, x_last) * a.ldx
+                                                              : w_rows + (int64_t)std::min((p - kXPieces) * kRows + r, w_last) * a.ldw;
+                            *reinterpret_cast<v4i *>(to + (p * kThreads + late) * 16) = load_16(from, BK * s + 16 * piece, a.k);
+                        }
                     }
                 }
             };
@@ -303,11 +324,12 @@ __global__ void __launch_bounds__(64 * WT * WC, RT * RC == 64 ? 1 : 2) dense_til
         settled_and_meet();
         // The wave's sums go through LDS of its own, 32 tokens at a time, so that its stores are whole
         // stretches of a token's channels.  A lane has the same four channels of every token.
+        const int late = again(t) & 63;         // the lane
         constexpr int kFours = 4 * RC, kTurns = 32 * kFours / 64;
-        static_assert(RT % 2 == 0 && 64 % kFours == 0, "32 tokens at a time, a lane the same channels");
+        static_assert(RT % 2 == 0 && 64 % kFours == 0, "32 tokens at a time, a late the same channels");
         int8_t *const my_place = wave / kPerPlace == 0 ? place_0 : wave / kPerPlace == 1 ? place_1 : wave / kPerPlace == 2 ? place_2 : place_3;
         int *own = reinterpret_cast<int *>(my_place) + wave % kPerPlace * 32 * kRow;
-        const int wave_t = (wave / WC) * 16 * RT, wave_c = (wave % WC) * 16 * RC + 4 * (lane % kFours);
+        const int wave_t = (wave / WC) * 16 * RT, wave_c = (wave % WC) * 16 * RC + 4 * (late % kFours);
         const int64_t j = j0 + wave_c;
         Channels channels;
         channels.left = a.n - j < 4 ? (int)(a.n - j) : 4;
@@ -319,20 +341,20 @@ __global__ void __launch_bounds__(64 * WT * WC, RT * RC == 64 ? 1 : 2) dense_til
             for (int half = 0; half < 2; ++half)
 #pragma unroll
                 for (int c = 0; c < RC; ++c)
-                    *reinterpret_cast<v4i *>(own + (16 * half + (lane & 15)) * kRow + 16 * c + 4 * (lane >> 4)) = acc[r + half][c];
+                    *reinterpret_cast<v4i *>(own + (16 * half + (late & 15)) * kRow + 16 * c + 4 * (late >> 4)) = acc[r + half][c];
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
             v4i sums[kTurns];
             float x_scale[kTurns];
 #pragma unroll
             for (int u = 0; u < kTurns; ++u) {
-                const int token = lane / kFours + 64 / kFours * u;
-                sums[u] = *reinterpret_cast<const v4i *>(own + token * kRow + 4 * (lane % kFours));
+                const int token = late / kFours + 64 / kFours * u;
+                sums[u] = *reinterpret_cast<const v4i *>(own + token * kRow + 4 * (late % kFours));
                 x_scale[u] = x_scales[wave_t + 16 * r + token];
             }
 #pragma unroll
             for (int u = 0; u < kTurns; ++u) {
-                const int64_t i = i0 + wave_t + 16 * r + lane / kFours + 64 / kFours * u;
+                const int64_t i = i0 + wave_t + 16 * r + late / kFours + 64 / kFours * u;
                 if (i < a.m && channels.left > 0) finish_4(a, i, j, sums[u], x_scale[u], channels);
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -348,10 +370,11 @@ template <int RT, int RC, int AHEAD, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES) dense_few_kernel(DenseClearArgs a) {
     static_assert(RT * RC <= WAVES, "a wave a tile of the sums");
     __shared__ v4i sums[WAVES][RT * RC][64];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const unsigned groups = (unsigned)((a.n + 16 * RC - 1) / (16 * RC));
-    const int blocks = a.k / 64, part = 16 * (lane >> 4);
+    const int blocks = a.k / 64;
     for (unsigned group = blockIdx.x; group < groups; group += gridDim.x) {
+        const int t = again(threadIdx.x), lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+        const int part = 16 * (lane >> 4);
         const int64_t first = (int64_t)group * 16 * RC;
         const int8_t *w[RC], *x[RT];
 #pragma unroll
@@ -470,7 +493,9 @@ static float tile_cost(const TileForm &f, const DenseClearArgs &a) {
     return last.fixed + last.step * steps + (float)rounds * (0.67f * full.fixed + full.step * steps);
 }
 
-static void dense_launch(const DenseClearArgs &a, hipStream_t stream) {
+static void dense_launch(DenseClearArgs a, hipStream_t stream) {
+    // An output larger than the eight L2s (4 MiB each) would only push the operands out of them: 8192 x 10240 -> 8192 617 -> 587 us, 8192 x 4096 -> 8192 272 -> 249.
+    a.past = a.m * a.n * (a.kind == BNN_CLEAR_F32 || a.kind == BNN_CLEAR_I32 ? 4 : a.kind <= BNN_CLEAR_F16 ? 2 : 1) > (int64_t)32 << 20;
     const auto fours = [](const void *p, int64_t ld) { return reinterpret_cast<uintptr_t>(p) % 4 == 0 && ld % 4 == 0 && ld <= 1 << 22; };
     const bool direct = fours(a.x, a.ldx) && fours(a.w, a.ldw);
     // Up to 16 tokens read each weight once; so do up to 32 if the channels are few enough that tiles would leave CUs idle
@@ -673,7 +698,7 @@ __global__ void __launch_bounds__(SPREAD ? 1024 : 256) rows_kernel(RowsClearArgs
          row += stride, turn ^= 1) {
         // what goes by the thread is found anew for each row: kept from row to row, the many addresses and conditions of more than two chunks
         // crowd values out of the registers
-        asm volatile("" : "+v"(own.t));
+        own.t = again(own.t);
         const T *pa = static_cast<const T *>(a.a) + row * a.lda, *pb = a.b ? static_cast<const T *>(a.b) + row * a.ldb : nullptr;
         const T *weight = static_cast<const T *>(a.weight);
         constexpr int kTogether = CHUNKS == 1 ? 1 : 2;     // chunks whose loads are under way at once, as registers allow

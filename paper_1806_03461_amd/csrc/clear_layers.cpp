@@ -106,7 +106,7 @@ extern "C" {
 int bnn_dense_clear(const int8_t *x, int64_t ldx, const int8_t *w, int64_t ldw, const float *x_scale, const float *w_scale,
                     const void *bias, void *out, int64_t ldo, int kind, int64_t m, int64_t n, int64_t k, void *stream) {
     return guarded([&]() -> int {
-        return dense_clear({x, w, x_scale, w_scale, bias, out, ldx, ldw, ldo, m, n, (int)k, kind}, k, stream);
+        return dense_clear({x, w, x_scale, w_scale, bias, out, ldx, ldw, ldo, m, n, (int)k, kind, false}, k, stream);
     });
 }
 

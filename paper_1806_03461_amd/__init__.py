@@ -365,9 +365,9 @@ def _clear_call(name, t):
     global _torch
     if _torch is None:
         _torch = _Torch()
-    if not t.is_cuda or t.dim() != 2:
-        raise ValueError(f"{name} must be a matrix on the GPU")
     device = t.get_device()
+    if device < 0 or t.dim() != 2:
+        raise ValueError(f"{name} must be a matrix on the GPU")
     if device != _torch.device():
         raise ValueError(f"{name} is on {t.device}, which is not the current device")
     return _torch, device

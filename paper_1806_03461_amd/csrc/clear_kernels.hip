@@ -498,9 +498,10 @@ static void dense_launch(DenseClearArgs a, hipStream_t stream) {
     a.past = a.m * a.n * (a.kind == BNN_CLEAR_F32 || a.kind == BNN_CLEAR_I32 ? 4 : a.kind <= BNN_CLEAR_F16 ? 2 : 1) > (int64_t)32 << 20;
     const auto fours = [](const void *p, int64_t ld) { return reinterpret_cast<uintptr_t>(p) % 4 == 0 && ld % 4 == 0 && ld <= 1 << 22; };
     const bool direct = fours(a.x, a.ldx) && fours(a.w, a.ldw);
-    // Up to 16 tokens read each weight once; so do up to 32 if the channels are few enough that tiles would leave CUs idle
-    // (24 tokens, 4096 -> 4096 8.2 us, tiles 10.7; 4096 -> 8192 12.8 and 11.1).
-    if (a.m <= 16) return few_launch<1, 1, 2, 8>(a, stream);
+    // Up to 16 tokens read each weight once.  From five tokens on each of its workgroups' reading of all tokens costs as much as the weights, and with more
+    // than two workgroups a CU tiles, which share it, take less (16 tokens, 4096 -> 8192 10.2 us, tiles 10.4; 4096 -> 12288 13.4 and 11.0; one token 10.4 and 10.8).
+    if (a.m <= 4 || (a.m <= 16 && (a.n <= 8192 || !direct))) return few_launch<1, 1, 2, 8>(a, stream);
+    // Up to 32 likewise, while channels are few enough that tiles leave CUs idle (32 tokens, 4096 -> 4096 8.5 us, tiles 10.2; 4096 -> 8192 12.8 and 10.8).
     if (a.m <= 32 && a.n <= 4096) return few_launch<2, 1, 4, 8>(a, stream);
     // Through registers the largest has none left (2001-byte rows, 4000 x 4000: 73 us, and 82 with the one before), rows a few bytes long aside.
     int form = 0;

@@ -43,7 +43,8 @@ static int dense_clear(const DenseClearArgs &a, int64_t k, void *stream) {
     if (int rc = check_stride("out", a.ldo, a.n)) return rc;
     if (a.kind >= BNN_CLEAR_I32 && (a.x_scale || a.w_scale)) return set_error(TFHE_E_PARAM, "whole-number outputs take no scales");
     if (a.m == 0 || a.n == 0) return TFHE_OK;
-    if ((a.m + 63) / 64 * ((a.n + 63) / 64) > INT32_MAX) return set_error(TFHE_E_SIZE, "%lld x %lld outputs are too many", (long long)a.m, (long long)a.n);
+    if ((a.m + 31) / 32 * ((a.n + 63) / 64) > INT32_MAX)      // the kernels count tiles in 32 bits
+         return set_error(TFHE_E_SIZE, "%lld x %lld outputs are too many", (long long)a.m, (long long)a.n);
     if (k > 0) {
         if (int rc = check_pointer("x", a.x, 1)) return rc;
         if (int rc = check_pointer("w", a.w, 1)) return rc;

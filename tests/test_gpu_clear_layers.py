@@ -114,6 +114,33 @@ def test_product_strides_and_alignment(T, shape, pads, leads):
         check_product(T, int8(g, m, k), int8(g, n, k), out, pads=pads, leads=leads, seed=n)
 
 
+KS = [4, 60, 64, 68, 128, 132, 192, 200, 256, 260, 320, 384, 392, 448, 452, 512, 576, 580, 640, 708, 768, 896, 1028, 1152, 1292]
+
+
+@pytest.mark.parametrize("m, n", [(11, 9001), (29, 300), (29, 5003), (97, 161), (4105, 69), (4625, 1665), (3285, 587), (898, 4435), (4663, 2562)])
+@pytest.mark.parametrize("more", [0, 1, 2, 12])
+def test_product_of_every_number_of_steps(T, m, n, more):
+    """Sizes at which each way to split the outputs is the one taken, none of them a whole number of its tiles, with k of none to twenty steps, whole and
+    not; rows at multiples of 4 and 16 bytes and at any address.  The sums are whole numbers below 2^53, which a product in 64 bits has exactly."""
+    g = torch.Generator(device="cuda").manual_seed(m + more)
+    for k in KS:
+        k += more
+        x, w = (torch.randint(-128, 128, (r, k), generator=g, device="cuda", dtype=torch.int8) for r in (m, n))
+        wide = torch.full((m + 1, n + 3), -7, dtype=torch.int32, device="cuda")
+        T.bnn_dense_clear(x, w, wide[:m, :n])
+        want = x.double() @ w.double().t()
+        assert torch.equal(wide[:m, :n].double(), want), k
+        assert bool((wide[m] == -7).all()) and bool((wide[:, n:] == -7).all()), k
+        if k % 64 < 8:
+            sx, sw, b = torch.rand(m, generator=g, device="cuda"), torch.rand(n, generator=g, device="cuda"), torch.randn(n, generator=g, device="cuda")
+            out = torch.empty(m, n, dtype=torch.float16, device="cuda")
+            T.bnn_dense_clear(x, w, out, x_scale=sx, w_scale=sw * 1e-3, bias=b)
+            y = want * sx.double()[:, None] * (sw * 1e-3).double()
+            full = y + b.double()
+            bound = 3 * U * y.abs() * (1 + 1e-6) + (U + 2.0 ** -11) * full.abs() * (1 + 2.0 ** -10) + 2.0 ** -25
+            assert bool(((out.double() - full).abs() <= bound).all()), k
+
+
 @pytest.mark.parametrize("m, n", [(1, 5), (20, 40), (100, 130), (300, 520)])
 def test_product_of_extremes(T, m, n):
     """-128 times -128 over the longest rows: the sum's last place before 2^31; and rows of all kinds of ends."""

@@ -129,9 +129,9 @@ __device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t from, int off
 // something of the row), so that eight lanes that read the same piece of eight rows meet all banks.
 // The channels are the products' rows: a lane then holds four neighbouring channels of a token.
 //   DIRECT: rows begin at multiples of 4 bytes, and pieces go from memory to LDS directly, but for the last step if k is no whole number of
-//   steps.  Otherwise all go through registers, two steps ahead.
+//   steps.  Otherwise all go through registers, two or four steps ahead.
 template <int WT, int WC, int RT, int RC, int BK, bool DIRECT>
-__global__ void __launch_bounds__(64 * WT * WC, RT * RC == 64 ? 1 : 2) dense_tile_kernel(DenseClearArgs a) {
+__global__ void __launch_bounds__(64 * WT * WC, 2) dense_tile_kernel(DenseClearArgs a) {
     constexpr int kThreads = 64 * WT * WC, kWaves = WT * WC, TT = 16 * WT * RT, TC = 16 * WC * RC;
     constexpr int kPerRow = BK / 16;                        // pieces a row
     constexpr int kRows = kThreads / kPerRow;               // rows of one piece a thread
@@ -326,7 +326,7 @@ __global__ void __launch_bounds__(64 * WT * WC, RT * RC == 64 ? 1 : 2) dense_til
         // stretches of a token's channels.  A lane has the same four channels of every token.
         const int late = again(t) & 63;         // the lane
         constexpr int kFours = 4 * RC, kTurns = 32 * kFours / 64;
-        static_assert(RT % 2 == 0 && 64 % kFours == 0, "32 tokens at a time, a late the same channels");
+        static_assert(RT % 2 == 0 && 64 % kFours == 0, "32 tokens at a time, a lane the same channels");
         int8_t *const my_place = wave / kPerPlace == 0 ? place_0 : wave / kPerPlace == 1 ? place_1 : wave / kPerPlace == 2 ? place_2 : place_3;
         int *own = reinterpret_cast<int *>(my_place) + wave % kPerPlace * 32 * kRow;
         const int wave_t = (wave / WC) * 16 * RT, wave_c = (wave % WC) * 16 * RC + 4 * (late % kFours);
@@ -366,6 +366,9 @@ __global__ void __launch_bounds__(64 * WT * WC, RT * RC == 64 ? 1 : 2) dense_til
 
 // Few tokens (up to 16 RT): the weights are read once and that is what it costs.  A workgroup takes 16 RC channels, its waves
 // consecutive parts of k, 64 bytes at a time; the weights go from memory to the products' registers without LDS, the waves' sums meet there.
+// Two blocks under way a wave leave registers for 28 waves a CU (one token, 10240 -> 4096 8.8 us, four 10.7, eight 10.0; 4096 -> 4096 5.5 us of which 2.5 are
+// the smallest call's: 16.8 MB at 5.6 TB/s).  Reading the weights past the caches' order of what to keep took 11.9 instead of 8.8: rows of
+// several calls stay in the 256 MB behind the L2s.
 template <int RT, int RC, int AHEAD, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES) dense_few_kernel(DenseClearArgs a) {
     static_assert(RT * RC <= WAVES, "a wave a tile of the sums");
@@ -507,7 +510,6 @@ static void dense_launch(DenseClearArgs a, hipStream_t stream) {
     int form = 0;
     for (int f = 1; f < (direct ? 6 : 5); ++f)
         if (tile_cost(kTileForms[f], a) < tile_cost(kTileForms[form], a)) form = f;
-    // FORM-END
     switch (form) {
         case 0: tile_launch<1, 4, 2, 1, 128>(a, direct, stream); break;
         case 1: tile_launch<2, 2, 2, 2, 128>(a, direct, stream); break;
@@ -535,7 +537,8 @@ struct Eight {
 // A row is read in chunks of eight values.  Each thread reads CHUNKS of them, whole ones without a branch -- a chunk that is not
 // there is read at the row's beginning and replaced by zeros -- so that all its loads are under way at once; the one thread that
 // holds the row's last, partial chunk reads it value by value afterwards.  The pointer is aligned to a value only: the device takes wide
-// accesses at any such address.  The values are read once, past the caches' order of what to keep: 4096 x 10240 pairs in 34 us instead of 39.
+// accesses at any such address.  The values are read once, past the caches' order of what to keep: a kernel that only reads 4096 x 10240 pairs and writes a byte
+// for each takes 34 us that way and 39 without.
 struct Chunks {
     int t, threads, k;
     __device__ __forceinline__ int at(int c) const { return 8 * (t + threads * c); }
@@ -635,10 +638,16 @@ __device__ __forceinline__ RowSums across_wave(RowSums s) {
     return all;
 }
 
+// a / b from 1 / b, the last place right: the product, and once what it leaves over.
+__device__ __forceinline__ float quotient(float a, float b, float one_by_b) {
+    const float q = a * one_by_b;
+    return fmaf(fmaf(-q, b, a), one_by_b, q);
+}
+
 // relu; silu(v) = v / (1 + e^-v); gelu(v) = v Phi(v).  With up to 4096 x 10240 values a prompt these are bound by their instructions as much as by
 // memory, so both are as short as their accuracy allows:
 //   silu: e^-v as 2^p, the product p = -v log2(e) with what it rounds off, since 2^p turns an absolute error of p into a relative one:
-//   about eight roundings at any v.  What is below 2^-119 may be 0.
+//   about six roundings at any v.  What is below 2^-119 may be 0.
 //   gelu: Phi(-a) = e^(-a^2/2) R(a) for a >= 0, R the scaled complementary error function; R as t P(t), t = 1 / (1 + 0.35 a), P
 //   the polynomial of degree 8 that a least-squares fit of the relative error at 400 Chebyshev points of t (a <= 15) gives: 3.6e-8 off, and 5
 //   roundings when evaluated in f32.  v Phi(v) is then max(v, 0) - |v| Phi(-|v|).  This keeps its relative accuracy far out on the negative
@@ -652,7 +661,8 @@ __device__ __forceinline__ float activated(float v) {
         const float h = __builtin_amdgcn_fmed3f(-v, -200.0f, 200.0f), p = h * kLog2e;
         const float r = fmaf(h, kRest, fmaf(h, kLog2e, -p));
         const float e = __builtin_amdgcn_exp2f(p) * fmaf(r, kLn2, 1.0f);
-        return v * __builtin_amdgcn_rcpf(1.0f + e);
+        const float d = 1.0f + e, by = __builtin_amdgcn_rcpf(d);
+        return d < 0x1p100f ? quotient(v, d, by) : v * by;
     } else {
         const float a = fminf(fabsf(v), 20.0f);
         const float e = __builtin_amdgcn_exp2f(a * a * -0.72134752f);
@@ -685,7 +695,7 @@ __device__ __forceinline__ void activate(int act, float (&v)[8]) {
 
 // A row a workgroup of up to sixteen waves (SPREAD), or a row a wave, four of them in a workgroup; the row's values are in registers from the
 // only reading to the rounding, CHUNKS chunks of eight a thread.
-//   norm: v = h * weight; y = v / rms, a positive number for the whole row, so that q = 127 v / max|v| needs no rms and one
+//   norm: v = h * weight; y = v / rms, a positive number for the whole row, so that q = v / (max|v| / 127) needs no rms and one
 //   reduction gives both the sum of squares and max|v|; only the scale, max|v| / (127 rms), takes it.
 //   gate: v = act(gate) * up.
 template <class T, bool NORM, bool SPREAD, int CHUNKS>
@@ -758,35 +768,32 @@ __global__ void __launch_bounds__(SPREAD ? 1024 : 256) rows_kernel(RowsClearArgs
             s = sums[turn][0];
             for (int w = 1; w < waves; ++w) s = join(s, sums[turn][w]);
         }
-        // q = 127 v / top
+        // q = v / step to the nearest, step = top / 127
+        constexpr float kPart = 1.0f / 127.0f;
         const float top = __uint_as_float(s.top);
-        float steps = 127.0f / top;
+        float step = top * kPart, per_step;
         if (__builtin_expect(!(s.top >= 0x0d800000u && s.top < 0x7f800000u), 0)) {
-            if (s.top != 0u && s.top < 0x7f800000u) {
-                // near the bottom of the f32 range (below 2^-100) 127 / top would be infinite: lifted by 2^100 first
-                steps = 127.0f / (top * 0x1p100f);
+            // near the bottom of the f32 range (below 2^-100) 1 / step would be infinite: lifted by 2^100 first.  Nothing but zeros, or
+            // something that is not a number: all 0
+            const bool lifted = s.top != 0u && s.top < 0x7f800000u;
+            step = lifted ? top * 0x1p100f * kPart : 0.0f;
+            per_step = lifted ? 1.0f / step : 0.0f;
 #pragma unroll
-                for (int c = 0; c < CHUNKS; ++c)
+            for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) v[c][j] *= 0x1p100f;
-            } else {
-                // nothing but zeros, or something that is not a number
-                steps = 0.0f;
-#pragma unroll
-                for (int c = 0; c < CHUNKS; ++c)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) v[c][j] = 0.0f;
-            }
+                for (int j = 0; j < 8; ++j) v[c][j] = lifted ? v[c][j] * 0x1p100f : 0.0f;
+        } else {
+            per_step = 1.0f / step;
         }
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
             unsigned bytes[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                // 1.5 * 2^23 added: the last byte of the sum is the product rounded to the nearest whole number, once
+                // 1.5 * 2^23 added: the last byte of the sum is the quotient rounded to the nearest whole number
                 unsigned w[4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) w[j] = __float_as_uint(fmaf(v[c][4 * h + j], steps, 12582912.0f));
+                for (int j = 0; j < 4; ++j) w[j] = __float_as_uint(quotient(v[c][4 * h + j], step, per_step) + 12582912.0f);
                 bytes[h] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(w[3], w[2], 0x0c0c0400u), __builtin_amdgcn_perm(w[1], w[0], 0x0c0c0400u), 0x05040100u);
             }
             Eight<int8_t> q;
@@ -794,9 +801,9 @@ __global__ void __launch_bounds__(SPREAD ? 1024 : 256) rows_kernel(RowsClearArgs
             write_8(a.q + row * a.ldq, q, own, c);
         }
         if (own.t == 0) {
-            double scale = (double)top / 127.0;
-            if (NORM) scale /= sqrt(s.squares / a.k + (double)a.eps);
-            a.scale[row] = a.k ? (float)scale : 0.0f;
+            float scale = top * kPart;
+            if constexpr (NORM) scale = (float)((double)top / (127.0 * sqrt(s.squares / a.k + (double)a.eps)));
+            a.scale[row] = a.k ? scale : 0.0f;
         }
     }
 }
@@ -813,8 +820,7 @@ static void rows_launch(const RowsClearArgs &a, hipStream_t stream) {
         rows_kernel<T, NORM, false, 1><<<groups_of((a.m + 3) / 4), 256, 0, stream>>>(a);
         return;
     }
-    int each = chunks <= 256 || (chunks <= 512 && a.m < 1024) ? 1 : chunks <= 1024 ? 2 : chunks <= 2048 ? (NORM || a.m < 512 ? 2 : 4) : chunks <= 4096 ? 4 : 8;
-    // ROWS
+    const int each = chunks <= 256 || (chunks <= 512 && a.m < 1024) ? 1 : chunks <= 1024 ? 2 : chunks <= 2048 ? (NORM || a.m < 512 ? 2 : 4) : chunks <= 4096 ? 4 : 8;
     const int threads = 64 * (((chunks + each - 1) / each + 63) / 64);
     switch (each) {
         case 1: rows_kernel<T, NORM, true, 1><<<groups_of(a.m), threads, 0, stream>>>(a); break;

@@ -407,7 +407,8 @@ def test_rows_more_than_a_launch_takes(T, m, k):
     q, scale = torch.empty(m, k, dtype=torch.int8, device="cuda"), torch.empty(m, device="cuda")
     T.bnn_gate_clear(x, None, "identity", q, scale)
     assert bool((q[:, 0] == 127).all()) and bool((q[:, 1] == 0).all()) and bool((q[:, k - 1] == 127).all())
-    assert torch.equal(scale, (x[:, 0].double() / 127).float())
+    want = x[:, 0].double() / 127       # 1 / 127 is rounded once, the product with it once
+    assert bool(((scale.double() - want).abs() <= 2 * U * (1 + U) * want).all())
 
 
 # ---- the operators together --------------------------------------------------------------------------------------------

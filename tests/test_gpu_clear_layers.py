@@ -201,6 +201,41 @@ def test_product_beyond_32_bits_of_offset(T):
     assert torch.equal(out.cpu(), (hw.int() @ hx.int().t()))
 
 
+def test_product_of_rows_far_apart(T):
+    """The widest strides that go straight to LDS, 4 MiB, and one beyond: a tile's rows span a gigabyte.  Largest tiles, ragged."""
+    m, n, k = 4663, 2562, 132
+    for ld in (2 ** 22, 2 ** 22 + 4):
+        g = torch.Generator(device="cuda").manual_seed(ld)
+        hx, hw = (torch.randint(-128, 128, (r, k), generator=g, device="cuda", dtype=torch.int8) for r in (m, n))
+        x, w = (torch.as_strided(torch.empty(ld * r, dtype=torch.int8, device="cuda"), (r, k), (ld, 1)) for r in (m, n))
+        x.copy_(hx)
+        w.copy_(hw)
+        out = torch.empty(m, n, dtype=torch.int32, device="cuda")
+        T.bnn_dense_clear(x, w, out)
+        assert torch.equal(out.double(), hx.double() @ hw.double().t())
+        del x, w
+    torch.cuda.empty_cache()
+
+
+def test_one_tensor_in_two_places(T):
+    """The same tensor as both operands of the product, as x and residual (and total), as gate and up."""
+    g = rng(6)
+    x = int8(g, 70, 200)
+    d, out = x.cuda(), torch.empty(70, 70, dtype=torch.int32, device="cuda")
+    T.bnn_dense_clear(d, d, out)
+    assert torch.equal(out.cpu(), x.int() @ x.int().t())
+    f = values(g, 7, 1500, torch.bfloat16)
+    q, scale, q2, scale2 = (torch.empty(7, 1500, dtype=torch.int8, device="cuda"), torch.empty(7, device="cuda"),
+                            torch.empty(7, 1500, dtype=torch.int8, device="cuda"), torch.empty(7, device="cuda"))
+    a, b = f.cuda(), f.cuda()
+    T.bnn_rms_norm_clear(a, None, 1e-5, q, scale, residual=a, total=a)
+    T.bnn_rms_norm_clear(b, None, 1e-5, q2, scale2, residual=f.cuda())
+    assert torch.equal(q, q2) and torch.equal(scale, scale2) and torch.equal(a.cpu(), 2 * f)
+    T.bnn_gate_clear(b, b, "silu", q, scale)
+    T.bnn_gate_clear(b, f.cuda(), "silu", q2, scale2)
+    assert torch.equal(q, q2) and torch.equal(scale, scale2)
+
+
 @pytest.mark.parametrize("m, n", [(68_000_000, 1), (3, 17_000_000)])
 def test_product_of_more_tiles_than_a_launch_takes(T, m, n):
     x = (torch.arange(m, device="cuda") % 251 - 125).to(torch.int8)[:, None]

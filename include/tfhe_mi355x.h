@@ -300,8 +300,9 @@ int bnn_dense_clear(const int8_t *x, int64_t ldx, const int8_t *w, int64_t ldw, 
  *   nearest whole number, ties to even.
  * x, residual, weight and total are of one type (F32, BF16 or F16); residual NULL: none; weight ([k]) NULL: ones; total, if not NULL,
  * receives h rounded to the type, and may be x or residual itself (same pointer and stride).  The norm is that of the unrounded h.
- * eps > 0.  k <= 32,768.  A row of zeros has scale 0 and q = 0.  A row in which h or h * weight leaves the f32 range or is
- * NaN has a scale that is not finite and q = 0: a product with it is not a number. */
+ * eps > 0.  k <= 32,768.  A row of zeros has scale 0 and q = 0.  h * weight is held in f32, so a row whose largest is not well above 2^-126
+ * loses digits there.  A row in which h or h * weight leaves the f32 range or is NaN has a scale that is not finite
+ * and q = 0: a product with it is not a number. */
 int bnn_rms_norm_clear(const void *x, int64_t ldx, const void *residual, int64_t ldr, const void *weight, float eps,
                        void *total, int64_t ldt, int8_t *q, int64_t ldq, float *scale, int type, int64_t m, int64_t k,
                        void *stream);

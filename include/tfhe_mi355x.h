@@ -296,8 +296,8 @@ int bnn_dense_clear(const int8_t *x, int64_t ldx, const int8_t *w, int64_t ldw, 
                     int64_t k, void *stream);
 
 /* Root-mean-square norm of rows, in 8 bits with a scale a row, what the product above takes:
- *   h = x + residual (f32);  y = h / sqrt(mean of h^2 + eps) * weight;  scale[i] = max |y| / 127;  q = y / scale[i] rounded to the
- *   nearest whole number, ties to even.
+ *   h = x + residual (f32);  y = h / sqrt(mean of h^2 + eps) * weight;  scale[i] = max |y| / 127;  q = y / scale[i], an f32 quotient,
+ *   rounded to the nearest whole number, ties to even.
  * x, residual, weight and total are of one type (F32, BF16 or F16); residual NULL: none; weight ([k]) NULL: ones; total, if not NULL,
  * receives h rounded to the type, and may be x or residual itself (same pointer and stride).  The norm is that of the unrounded h.
  * eps > 0.  k <= 32,768.  A row of zeros has scale 0 and q = 0.  h * weight is held in f32, so a row whose largest is not well above 2^-126

@@ -768,15 +768,16 @@ __global__ void __launch_bounds__(SPREAD ? 1024 : 256) rows_kernel(RowsClearArgs
             s = sums[turn][0];
             for (int w = 1; w < waves; ++w) s = join(s, sums[turn][w]);
         }
-        // q = v / step to the nearest, step = top / 127
+        // q = v / step to the nearest, step = top / 127 to the nearest: the product with 1 / 127 alone is a step of f32 off for one row in twenty, which
+        // moves values at half the largest (63.5 steps, common in rows of few bits) to the other side of their border
         constexpr float kPart = 1.0f / 127.0f;
         const float top = __uint_as_float(s.top);
-        float step = top * kPart, per_step;
+        float step = quotient(top, 127.0f, kPart), per_step;
         if (__builtin_expect(!(s.top >= 0x0d800000u && s.top < 0x7f800000u), 0)) {
             // near the bottom of the f32 range (below 2^-100) 1 / step would be infinite: lifted by 2^100 first.  Nothing but zeros, or
             // something that is not a number: all 0
             const bool lifted = s.top != 0u && s.top < 0x7f800000u;
-            step = lifted ? top * 0x1p100f * kPart : 0.0f;
+            step = lifted ? quotient(top * 0x1p100f, 127.0f, kPart) : 0.0f;
             per_step = lifted ? 1.0f / step : 0.0f;
 #pragma unroll
             for (int c = 0; c < CHUNKS; ++c)
@@ -801,7 +802,7 @@ __global__ void __launch_bounds__(SPREAD ? 1024 : 256) rows_kernel(RowsClearArgs
             write_8(a.q + row * a.ldq, q, own, c);
         }
         if (own.t == 0) {
-            float scale = top * kPart;
+            float scale = top / 127.0f;     // below 2^-100, and for what is not a number, too
             if constexpr (NORM) scale = (float)((double)top / (127.0 * sqrt(s.squares / a.k + (double)a.eps)));
             a.scale[row] = a.k ? scale : 0.0f;
         }

@@ -345,6 +345,8 @@ def bnn_conv_encrypted(ck, x, C_, H, Wd, K, T, stride, pad, out, stream=None):
 # Operands are torch tensors on the current device; rows may be strided, values of a row are neighbours.  A call of a few
 # microseconds is mostly this marshalling, so a tensor is looked at once and with the cheapest questions; torch's own
 # current_stream() alone takes 2.7 us, the handle it wraps 0.1.
+# The calls have no gradients: while torch records them, an operand that asks for one is refused rather than cut off from its graph.
+# What a call writes gets a new version, so that a backward pass that saved the values before says so.  The two take 0.35 to 0.5 us.
 
 class _Torch:
     """What these calls need of torch, looked up at the first of them."""
@@ -352,6 +354,7 @@ class _Torch:
     def __init__(self):
         import torch
         self.device, self.stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+        self.records, self.written = torch.is_grad_enabled, torch.autograd.graph.increment_version
         self.i8, self.i32, self.f32 = torch.int8, torch.int32, torch.float32
         self.kinds = {torch.float32: CLEAR_F32, torch.bfloat16: CLEAR_BF16, torch.float16: CLEAR_F16,
                       torch.int32: CLEAR_I32, torch.int8: CLEAR_SIGN, torch.uint8: CLEAR_BITS}
@@ -373,11 +376,18 @@ def _clear_call(name, t):
     return _torch, device
 
 
+def _without_gradient(name):
+    if _torch.records():
+        raise ValueError(f"{name} asks for a gradient, and this call has none: detach it, or call under torch.no_grad()")
+
+
 def _matrix(name, t, dtype, shape, device):
     """Device pointer and row stride of a [rows][width] tensor."""
     if t.dtype is not dtype or t.shape != shape or t.get_device() != device:
         raise ValueError(f"{name} must be a {shape[0]} x {shape[1]} tensor of {dtype} on device {device}, "
                          f"not {tuple(t.shape)} of {t.dtype} on {t.device}")
+    if t.requires_grad:
+        _without_gradient(name)
     if t.is_contiguous():
         return t.data_ptr(), shape[1]
     step, nxt = t.stride()
@@ -389,6 +399,8 @@ def _matrix(name, t, dtype, shape, device):
 def _vector(name, t, dtype, size, device):
     if t.dtype is not dtype or t.shape != (size,) or t.get_device() != device or not t.is_contiguous():
         raise ValueError(f"{name} must be {size} neighbouring values of {dtype} on device {device}")
+    if t.requires_grad:
+        _without_gradient(name)
     return t.data_ptr()
 
 
@@ -412,6 +424,7 @@ def bnn_dense_clear(x, w, out, x_scale=None, w_scale=None, bias=None, stream=Non
                                          t.stream(device) if stream is None else stream)
     if rc:
         _check(rc)
+    t.written(out)
 
 
 def bnn_rms_norm_clear(x, weight, eps, q, scale, residual=None, total=None, stream=None):
@@ -430,6 +443,7 @@ def bnn_rms_norm_clear(x, weight, eps, q, scale, residual=None, total=None, stre
                                             t.stream(device) if stream is None else stream)
     if rc:
         _check(rc)
+    t.written((q, scale) if total is None else (q, scale, total))
 
 
 def bnn_gate_clear(gate, up, act, q, scale, stream=None):
@@ -446,6 +460,7 @@ def bnn_gate_clear(gate, up, act, q, scale, stream=None):
                                         t.kinds.get(dtype, -1), m, k, t.stream(device) if stream is None else stream)
     if rc:
         _check(rc)
+    t.written((q, scale))
 
 
 def tfhe_plan_wire_pool(gates, nwires, n_fixed, outs):

@@ -309,7 +309,8 @@ int bnn_rms_norm_clear(const void *x, int64_t ldx, const void *residual, int64_t
 
 /* What stands between the two products of a gated feed-forward block: y = act(gate) * up in f32, or act(gate) if up is NULL, to 8 bits
  * with a scale a row as above.  gate and up may be the two halves of one product's output.  With BNN_ACT_IDENTITY
- * and no up this turns rows of numbers into what the product takes.  k <= 65,536. */
+ * and no up this turns rows of numbers into what the product takes.  k <= 65,536.  y is held in f32: SILU and GELU below 2^-119 lose digits or are 0,
+ * and so does the scale of a row whose largest is not well above 2^-119 (q goes by max |y| / 127 itself there). */
 int bnn_gate_clear(const void *gate, int64_t ldg, const void *up, int64_t ldu, int act, int8_t *q, int64_t ldq,
                    float *scale, int type, int64_t m, int64_t k, void *stream);
 

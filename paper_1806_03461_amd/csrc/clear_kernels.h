@@ -32,7 +32,8 @@ struct RowsClearArgs {
 
 // largest k of a product: 128 * 128 * k stays below 2^31
 constexpr int64_t kMaxDenseClearK = 131071;
-// longest rows: 1,024 threads hold one in registers, the norm's 32 values each, the gate's 64
+// longest rows: 1,024 threads hold one in registers, the norm's 32 values each, the gate's 64.  With 64 the norm, which holds weights and a second output beside
+// them, needs 200 bytes a lane of scratch, which the runtime would allocate at its first launch.
 constexpr int64_t kMaxNormClear = 32768, kMaxGateClear = 65536;
 
 int launch_dense_clear(const DenseClearArgs &a, hipStream_t stream);

@@ -366,9 +366,11 @@ __global__ void __launch_bounds__(64 * WT * WC, 2) dense_tile_kernel(DenseClearA
 
 // Few tokens (up to 16 RT): the weights are read once and that is what it costs.  A workgroup takes 16 RC channels, its waves
 // consecutive parts of k, 64 bytes at a time; the weights go from memory to the products' registers without LDS, the waves' sums meet there.
-// Two blocks under way a wave leave registers for 28 waves a CU (one token, 10240 -> 4096 8.8 us, four 10.7, eight 10.0; 4096 -> 4096 5.5 us of which 2.5 are
-// the smallest call's: 16.8 MB at 5.6 TB/s).  Reading the weights past the caches' order of what to keep took 11.9 instead of 8.8: rows of
-// several calls stay in the 256 MB behind the L2s.
+// Two blocks under way a wave leave registers for 28 waves a CU (one token, 10240 -> 4096 8.8 us, four 10.7, eight 10.0).
+// One token on weights that the 256 MB behind the L2s keep from one call to the next, and on weights from memory (a ring of 640 MB), the smallest call being
+// 2.0 us: 4096 -> 4096 4.9 and 6.5 us, 10240 -> 4096 8.6 and 11.2, 4096 -> 131072, which they cannot keep, 89, 6.0 TB/s.  Reading the weights past
+// the caches' order of what to keep takes 5.9 instead of 6.5 for 4096 -> 4096 from memory, but 9.9 instead of 8.6 for 10240 -> 4096 from the caches, 99 instead of 92 for 131072
+// channels and 29.7 instead of 26.7 for 16 tokens, 10240 -> 8192, from memory.
 template <int RT, int RC, int AHEAD, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES) dense_few_kernel(DenseClearArgs a) {
     static_assert(RT * RC <= WAVES, "a wave a tile of the sums");
@@ -476,6 +478,8 @@ static void tile_launch(const DenseClearArgs &a, bool direct, hipStream_t stream
 // The tile kernel's forms, and what a launch of each takes: with up to 256, 512, 768 tiles -- one, two, three on a CU, as many as its LDS
 // holds -- a start and end of `fixed` and `step` for 128 bytes of k, in us, measured as kernels of 4096-byte and 1024-byte rows in a
 // captured sequence.  More tiles than a device holds at once go round, a round after the first at the cost of its steps and two thirds of its start.
+// Over 60 random sizes the choice takes 2 % more than the best of the six on average, and 30 % at most (3045 x 320 -> 3968, three rounds of 128 x 128 tiles for one of
+// 256 x 256, 25.3 and 19.4 us).
 struct TileForm {
     int tokens, channels, at_once;
     struct { float fixed, step; } cost[3];
@@ -502,9 +506,11 @@ static void dense_launch(DenseClearArgs a, hipStream_t stream) {
     const auto fours = [](const void *p, int64_t ld) { return reinterpret_cast<uintptr_t>(p) % 4 == 0 && ld % 4 == 0 && ld <= 1 << 22; };
     const bool direct = fours(a.x, a.ldx) && fours(a.w, a.ldw);
     // Up to 16 tokens read each weight once.  From five tokens on each of its workgroups' reading of all tokens costs as much as the weights, and with more
-    // than two workgroups a CU tiles, which share it, take less (16 tokens, 4096 -> 8192 10.2 us, tiles 10.4; 4096 -> 12288 13.4 and 11.0; one token 10.4 and 10.8).
+    // than two workgroups a CU tiles, which share it, take less (16 tokens, 4096 -> 8192 10.0 us, tiles 9.9; 4096 -> 12288 13.4 and 11.0; 10240 -> 10240 29.3 and 20.8,
+    // from memory 36.8 and 32.9; one token, 4096 -> 10240 9.5 and 10.6, from memory 12.2 and 15.8).
     if (a.m <= 4 || (a.m <= 16 && (a.n <= 8192 || !direct))) return few_launch<1, 1, 2, 8>(a, stream);
-    // Up to 32 likewise, while channels are few enough that tiles leave CUs idle (32 tokens, 4096 -> 4096 8.5 us, tiles 10.2; 4096 -> 8192 12.8 and 10.8).
+    // Up to 32 likewise, while channels are few enough that tiles leave CUs idle.  Weights from memory decide it
+    // (32 tokens, 1024 -> 4096 5.0 us, tiles 6.8; 10240 -> 1024 19.1 and 30.0; 10240 -> 4096 20.5 and 30.9; 4096 -> 4096 9.7 and 14.8, where on kept weights it is 8.3 and 6.7).
     if (a.m <= 32 && a.n <= 4096) return few_launch<2, 1, 4, 8>(a, stream);
     // Through registers the largest has none left (2001-byte rows, 4000 x 4000: 73 us, and 82 with the one before), rows a few bytes long aside.
     int form = 0;
@@ -638,7 +644,9 @@ __device__ __forceinline__ RowSums across_wave(RowSums s) {
     return all;
 }
 
-// a / b from 1 / b, the last place right: the product, and once what it leaves over.
+// a / b from 1 / b: the product, and once what it leaves over (Markstein's correction).  Where one_by_b is 1 / b to the nearest, as for the rows'
+// steps, this is the quotient to the nearest (the same as a division for 4e8 random pairs, and for every a and b = 127); with a reciprocal one unit off, which
+// the hardware's may be, as in silu, it is one unit off for a pair in 100,000.
 __device__ __forceinline__ float quotient(float a, float b, float one_by_b) {
     const float q = a * one_by_b;
     return fmaf(fmaf(-q, b, a), one_by_b, q);

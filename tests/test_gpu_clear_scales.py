@@ -62,3 +62,19 @@ def test_every_leading_digit_of_a_largest_value(T):
         T.bnn_gate_clear(x.cuda(), None, "identity", q, scale)
         want_q, want = by_formula(x.float())
         assert torch.equal(scale.cpu(), want) and torch.equal(q.cpu(), want_q), (int((scale.cpu() != want).sum()), int((q.cpu() != want_q).sum()))
+
+
+def test_rows_at_the_bottom_of_f32(T):
+    """Largest values from 2^-149 to 2^-90: q goes by max / 127 itself, the scale is that number to the nearest f32, of few digits or none down there."""
+    g = torch.Generator().manual_seed(3)
+    top = torch.exp2(torch.linspace(-149, -90, 4000, dtype=torch.float64))
+    x = (top[:, None] * (2 * torch.rand(4000, 300, generator=g, dtype=torch.float64) - 1)).float()
+    x[:, 7] = top.float()
+    q, scale = torch.empty(4000, 300, dtype=torch.int8, device="cuda"), torch.empty(4000, device="cuda")
+    T.bnn_gate_clear(x.cuda(), None, "identity", q, scale)
+    want = x[:, 7].double() / 127
+    assert torch.equal(scale.cpu(), want.float())
+    real = x.double() / want[:, None]
+    # the step is one rounding of max / 127 and the quotient by it another, 127 * 2^-23 at most
+    assert bool(((q.cpu().double() - real).abs() <= 0.5 + 127 * 2.0 ** -23).all())
+    assert bool((q.cpu()[:, 7] == 127).all())
